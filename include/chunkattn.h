@@ -63,7 +63,14 @@ typedef enum {
   CA_ERR_HOST = -7       /* a host memory allocation inside the library failed */
 } ca_status;
 
-typedef enum { CA_FP16 = 0, CA_FP32 = 1 } ca_dtype;
+/* CA_FP16_KV4: q, o and the rows given to the cache are fp16, K and V are held
+ * in 4 bits. A row of d elements of one token and head stands for
+ * low + scale * code_i: low is the row's minimum, scale the fp16 rounding of
+ * (maximum - low) / 15 (an fp32 quotient), and code_i in 0..15 the nearest
+ * code, ties to even (0 throughout where scale is 0). A row with a non-finite
+ * element stands for NaN throughout. Attention computes with these values;
+ * the codes of a row never change once written. */
+typedef enum { CA_FP16 = 0, CA_FP32 = 1, CA_FP16_KV4 = 2 } ca_dtype;
 
 /*
  * Cache configuration (Section 3.1: chunk size c; the experiments use h=32,
@@ -71,7 +78,7 @@ typedef enum { CA_FP16 = 0, CA_FP32 = 1 } ca_dtype;
  *   chunk_size  c >= 1 tokens per chunk
  *   num_heads   H >= 1
  *   head_dim    d in {64, 128}
- *   dtype       element type of K, V, q and o
+ *   dtype       element type of K, V, q and o (see ca_dtype)
  *   num_slots   number of chunk slots in each pool (>= 1)
  *   k_pool, v_pool  caller-owned device buffers, 16-byte aligned. The K rows
  *               of chunk slot s, head h are the c*d contiguous elements at
@@ -90,6 +97,10 @@ typedef enum { CA_FP16 = 0, CA_FP32 = 1 } ca_dtype;
  *               + c*d elements. Example: the interleaved layout
  *               [slot][head][K|V][c][d] in one buffer is v_pool = k_pool + c*d,
  *               head_stride = 2*c*d, slot_stride = 2*H*c*d.
+ *               CA_FP16_KV4: strides are in bytes and a tile takes
+ *               ceil(c/16) * 16 * (d/2 + 4) bytes in place of c*d elements
+ *               (codes, then a scale and a low per row; the arrangement
+ *               inside a tile is the library's own).
  */
 typedef struct {
   int32_t chunk_size;
@@ -242,6 +253,44 @@ ca_status ca_attention_ordered(ca_cache* cache, const void* q, void* o, const in
  * B == 0 is a no-op. */
 ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float scale, void* stream);
 
+/* Decode attention with a sliding window and sinks. The query of a sequence
+ * of length L sits at position L - 1 and sees the positions j < L with
+ * j < sinks or j >= L - window:
+ *   o = sum_j softmax_j(scale q.k_j) v_j over those j.
+ * All of ca_dtype; what is not seen is not read, and its values (also NaN or
+ * infinite ones) do not reach o.
+ *   seq_ids, n   host, the rows' order as in ca_attention_ordered; NULL: tree
+ *                row order (n is ignored)
+ *   window       >= 1 positions, the query's own among them; sinks >= 0 first
+ *                positions that stay visible
+ *   ws           device workspace of ws_bytes >= ca_window_workspace_size()
+ *                bytes for the same window and sinks, 256-byte aligned
+ *   q, o, scale, stream   as ca_attention
+ * The kernel context of a window is built for the current tree when first
+ * asked for and patched or rebuilt after structural changes, as ca_attention's
+ * is; a cache keeps the contexts of the last two (window, sinks) pairs. It
+ * holds the chunks that a window reached when it was built or last patched,
+ * and lengths are read on the device, so appends that only fill chunks need
+ * no upload. ca_set_tuning does not apply. While `stream` is being captured
+ * into a graph nothing is allocated or uploaded: INVALID is returned unless
+ * ca_prepare_window and one call (for the counters) came before.
+ * Errors: INVALID (table-only cache, null or misaligned q/o, bad scale,
+ * window or sinks, bad seq_ids, context not current under capture),
+ * WORKSPACE, DEVICE. No live sequence is a no-op. */
+ca_status ca_attention_window(ca_cache* cache, const void* q, void* o, const int64_t* seq_ids, int64_t n,
+                              int64_t window, int64_t sinks, float scale, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* Bytes of device workspace ca_attention_window needs for the current tree
+ * (0 is possible). For a CA_FP16_KV4 cache ca_workspace_size is this for a
+ * window past every length. Errors: INVALID. */
+ca_status ca_window_workspace_size(const ca_cache* cache, int64_t window, int64_t sinks, size_t* bytes);
+
+/* ca_prepare for ca_attention_window's kernel context of (window, sinks).
+ * Errors: INVALID, DEVICE. */
+ca_status ca_prepare_window(ca_cache* cache, int64_t window, int64_t sinks, void* stream,
+                            int32_t* uploaded);
+
 /* Bring the kernel context up to date now (Section 3.3, further
  * optimizations: context generation hidden behind earlier GPU work). Builds
  * the tables and work lists for the current tree on the host and, if they
@@ -336,6 +385,8 @@ ca_status ca_stats(const ca_cache* cache, int64_t* uploads, int64_t* slots_used,
  *                default 7 runs all). A subset is for timing one kernel in
  *                isolation and leaves o incomplete unless the other phases'
  *                results are already in the workspace.
+ * A CA_FP16_KV4 cache's calls run over plans of their own (see
+ * ca_attention_window) and do not follow these settings.
  * Changing seg_chunks, split_chunks or schedule rebuilds the kernel context and
  * may change ca_workspace_size. Errors: INVALID. */
 ca_status ca_set_tuning(ca_cache* cache, int32_t seg_chunks, int32_t split_chunks,

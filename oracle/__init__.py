@@ -19,7 +19,10 @@ It is a plain, slow, obviously-correct restatement of ChunkAttention
                  self-check only, the same result assembled chunk by chunk with
                  partial_attn (Eqn 1) and attn_reduce (Eqn 2); plus causal
                  prefill attention for a sequence's last tokens over its
-                 whole path (Section 3.2, prefill paragraph).
+                 whole path (Section 3.2, prefill paragraph);
+  * ``window`` - the same attention where a query sees a sliding window and
+                 the first few positions only;
+  * ``kv4``    - the values that rows of a cache held in 4 bits stand for.
 """
 from .tree import OracleTree, PoolExhausted  # noqa: F401
 from .tables import tables, Tables  # noqa: F401
@@ -32,3 +35,5 @@ from .attention import (  # noqa: F401
     path_kv,
     prefill_attention,
 )
+from .kv4 import kv4_quantise, kv4_values  # noqa: F401
+from .window import visible, window_attention, window_prefill  # noqa: F401

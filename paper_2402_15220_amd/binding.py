@@ -31,10 +31,13 @@ STATUS_NAMES = {0: "OK", -1: "INVALID", -2: "NOMEM", -3: "NOT_FOUND", -4: "EXIST
 
 CA_FP16 = 0
 CA_FP32 = 1
+CA_FP16_KV4 = 2
 
 EXPORTED = ["ca_create", "ca_destroy", "ca_match", "ca_insert", "ca_extend", "ca_append_batch",
             "ca_remove", "ca_num_seqs", "ca_seq_order", "ca_workspace_size", "ca_attention",
-            "ca_attention_ordered", "ca_attention_noalloc", "ca_prefill_attention", "ca_prepare", "ca_export_tables", "ca_stats", "ca_set_tuning", "ca_last_error"]
+            "ca_attention_ordered", "ca_attention_noalloc", "ca_attention_window",
+            "ca_window_workspace_size", "ca_prepare_window", "ca_prefill_attention", "ca_prepare",
+            "ca_export_tables", "ca_stats", "ca_set_tuning", "ca_last_error"]
 
 
 class ChunkAttnError(RuntimeError):
@@ -93,6 +96,9 @@ def load():
         "ca_prepare": [vp, vp, ctypes.POINTER(i32)],
         "ca_attention_ordered": [vp, vp, vp, _P64, i64, ctypes.c_float, vp, ctypes.c_size_t, vp],
         "ca_attention_noalloc": [vp, vp, vp, ctypes.c_float, vp],
+        "ca_attention_window": [vp, vp, vp, _P64, i64, i64, i64, ctypes.c_float, vp, ctypes.c_size_t, vp],
+        "ca_window_workspace_size": [vp, i64, i64, ctypes.POINTER(ctypes.c_size_t)],
+        "ca_prepare_window": [vp, i64, i64, vp, ctypes.POINTER(i32)],
         "ca_export_tables": [vp, ctypes.POINTER(CaTables)],
         "ca_stats": [vp, _P64, _P64, _P64, ctypes.POINTER(i32), ctypes.POINTER(i32), _P64],
         "ca_set_tuning": [vp, i32, i32, i32, i32],
@@ -204,6 +210,29 @@ def ca_attention_ordered(h, q, o, seq_ids, scale, ws, ws_bytes, stream=None):
 
 def ca_attention_noalloc(h, q, o, scale, stream=None):
     _check(load().ca_attention_noalloc(h, q, o, ctypes.c_float(scale), stream))
+
+
+def ca_attention_window(h, q, o, seq_ids, window, sinks, scale, ws, ws_bytes, stream=None):
+    """seq_ids None: tree row order."""
+    ids, ip, n = None, None, 0
+    if seq_ids is not None:
+        ids, ip = _i64(seq_ids)
+        n = ids.shape[0]
+    _check(load().ca_attention_window(h, q, o, ip, n, window, sinks, ctypes.c_float(scale), ws,
+                                      ws_bytes, stream))
+
+
+def ca_window_workspace_size(h, window, sinks) -> int:
+    n = ctypes.c_size_t()
+    _check(load().ca_window_workspace_size(h, window, sinks, ctypes.byref(n)))
+    return n.value
+
+
+def ca_prepare_window(h, window, sinks, stream=None) -> bool:
+    """True if an upload of the window's kernel context was enqueued."""
+    up = ctypes.c_int32()
+    _check(load().ca_prepare_window(h, window, sinks, stream, ctypes.byref(up)))
+    return bool(up.value)
 
 
 def ca_prepare(h, stream=None) -> bool:

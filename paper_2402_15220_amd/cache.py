@@ -26,33 +26,53 @@ class Cache:
     every decode workload, most on calls that miss the caches); ``"split"``
     uses two buffers [slot][head][c][d] (the C ABI's dense default).
     ``k_pool``/``v_pool`` are [slot][head][c][d] views either way.
+
+    ``kv_bits=4`` (fp16 only) holds K and V in 4 bits: a row of one token and
+    head stands for ``low + scale * code`` with 16 codes between its minimum
+    and maximum (``CA_FP16_KV4`` in the C header). Rows are given, and q and o
+    are, in fp16 all the same; pools are uint8, [slot][head][tile bytes].
     """
 
     def __init__(self, chunk_size: int, num_heads: int, head_dim: int, num_slots: int,
                  dtype=torch.float16, device="cuda", table_only: bool = False,
-                 layout: str = "interleaved"):
+                 layout: str = "interleaved", kv_bits: int | None = None):
+        if kv_bits not in (None, 4) or (kv_bits == 4 and dtype != torch.float16):
+            raise ValueError("kv_bits is None (rows kept in dtype) or 4 (with dtype float16)")
         self.c, self.H, self.d = chunk_size, num_heads, head_dim
         self.dtype = dtype
+        self.kv_bits = kv_bits
+        code = B.CA_FP16_KV4 if kv_bits == 4 else _DT[dtype]
         self.num_slots = num_slots
         self.table_only = table_only
         self.layout = None if table_only else layout
         if table_only:
             self.k_pool = self.v_pool = None
-            self.h = B.ca_create(chunk_size, num_heads, head_dim, _DT[dtype], num_slots)
+            self.h = B.ca_create(chunk_size, num_heads, head_dim, code, num_slots)
+        elif kv_bits == 4 and layout in ("interleaved", "split"):
+            tile = -(-chunk_size // 16) * 16 * (head_dim // 2 + 4)  # bytes
+            if layout == "interleaved":
+                self.kv_pool = torch.empty((num_slots, num_heads, 2, tile), dtype=torch.uint8, device=device)
+                self.k_pool, self.v_pool = self.kv_pool[:, :, 0], self.kv_pool[:, :, 1]
+            else:
+                self.k_pool, self.v_pool = (torch.empty((num_slots, num_heads, tile), dtype=torch.uint8,
+                                                        device=device) for _ in range(2))
+            self.h = B.ca_create(chunk_size, num_heads, head_dim, code, num_slots,
+                                 self.k_pool.data_ptr(), self.v_pool.data_ptr(),
+                                 slot_stride=self.k_pool.stride(0), head_stride=self.k_pool.stride(1))
         elif layout == "interleaved":
             self.kv_pool = torch.empty((num_slots, num_heads, 2, chunk_size, head_dim), dtype=dtype,
                                        device=device)
             self.k_pool = self.kv_pool[:, :, 0]
             self.v_pool = self.kv_pool[:, :, 1]
             tile = chunk_size * head_dim
-            self.h = B.ca_create(chunk_size, num_heads, head_dim, _DT[dtype], num_slots,
+            self.h = B.ca_create(chunk_size, num_heads, head_dim, code, num_slots,
                                  self.k_pool.data_ptr(), self.v_pool.data_ptr(),
                                  slot_stride=2 * num_heads * tile, head_stride=2 * tile)
         elif layout == "split":
             shape = (num_slots, num_heads, chunk_size, head_dim)
             self.k_pool = torch.empty(shape, dtype=dtype, device=device)
             self.v_pool = torch.empty(shape, dtype=dtype, device=device)
-            self.h = B.ca_create(chunk_size, num_heads, head_dim, _DT[dtype], num_slots,
+            self.h = B.ca_create(chunk_size, num_heads, head_dim, code, num_slots,
                                  self.k_pool.data_ptr(), self.v_pool.data_ptr())
         else:
             raise ValueError(f"unknown layout {layout!r}")
@@ -125,21 +145,37 @@ class Cache:
     def set_tuning(self, seg_chunks=0, split_chunks=-1, phase_mask=0, schedule=-1):
         B.ca_set_tuning(self.h, seg_chunks, split_chunks, phase_mask, schedule)
 
-    def prepare(self) -> bool:
-        """Build the kernel context for the current tree now and enqueue its
-        upload on the current stream (True if one was needed)."""
-        return B.ca_prepare(self.h, None if self.table_only else self.stream())
+    def prepare(self, window: int | None = None, sinks: int = 0) -> bool:
+        """Build the kernel context for the current tree now (of attention with
+        that window, if one is given) and enqueue its upload on the current
+        stream (True if one was needed)."""
+        s = None if self.table_only else self.stream()
+        if self._window(window, sinks):
+            return B.ca_prepare_window(self.h, window, sinks, s)
+        return B.ca_prepare(self.h, s)
 
     # -- attention ---------------------------------------------------------
-    def workspace(self):
-        need = B.ca_workspace_size(self.h)
+    def _window(self, window, sinks) -> bool:
+        """Whether a window is asked for (the library checks its values)."""
+        if window is None and sinks != 0:
+            raise ValueError("sinks need a window")
+        return window is not None
+
+    def workspace(self, window: int | None = None, sinks: int = 0):
+        if self._window(window, sinks):
+            need = B.ca_window_workspace_size(self.h, window, sinks)
+        else:
+            need = B.ca_workspace_size(self.h)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k_pool.device)
         return self._ws, need
 
-    def attention(self, q, out=None, scale: float = 0.0, seq_ids=None):
+    def attention(self, q, out=None, scale: float = 0.0, seq_ids=None, window: int | None = None,
+                  sinks: int = 0):
         """q: [B, H, d] in seq_order(), or in the order of ``seq_ids`` (every
-        live sequence once) when given; returns o in the same row order."""
+        live sequence once) when given; returns o in the same row order.
+        ``window``: a sequence of L tokens sees its last ``window`` positions and
+        its first ``sinks``; without it, all."""
         if self.table_only:
             raise ValueError("table-only cache has no attention")
         Bn = self.num_seqs()
@@ -147,8 +183,11 @@ class Cache:
         if out is None:
             out = torch.empty_like(q)
         self._check_rows(out, Bn, "out")
-        ws, need = self.workspace()
-        if seq_ids is None:
+        ws, need = self.workspace(window, sinks)
+        if window is not None:
+            B.ca_attention_window(self.h, q.data_ptr(), out.data_ptr(), seq_ids, window, sinks, scale,
+                                  ws.data_ptr(), ws.numel(), self.stream())
+        elif seq_ids is None:
             B.ca_attention(self.h, q.data_ptr(), out.data_ptr(), scale, ws.data_ptr(), ws.numel(),
                            self.stream())
         else:

@@ -14,6 +14,8 @@
 
 #include "../../include/chunkattn.h"
 #include "kernels.hpp"
+#include "kv4.hpp"
+#include "plan.hpp"
 #include "tables.hpp"
 #include "tree.hpp"
 
@@ -142,6 +144,29 @@ ca_status ensure_device(char** p, size_t* cap, size_t need, hipStream_t stream, 
   return CA_OK;
 }
 
+// A stream whose work is being recorded into a graph: no allocation and no
+// copy from staging memory may be enqueued on it.
+bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &st) != hipSuccess) {
+    (void)hipGetLastError();
+    return false;
+  }
+  return st != hipStreamCaptureStatusNone;
+}
+
+// A decode plan (plan.hpp) and its device copy.
+struct PlanSlot {
+  ca::Plan plan;
+  bool valid = false;     // matches the tree
+  bool uploaded = false;  // the device copy matches the plan
+  uint64_t used = 0;      // when it was last asked for
+  char* d = nullptr;
+  size_t cap = 0;
+  size_t o_chunks = 0, o_rows = 0;  // offsets in the device copy
+  PinnedStaging stage;
+};
+
 }  // namespace
 
 struct ca_cache {
@@ -187,6 +212,11 @@ struct ca_cache {
   char* scratch = nullptr;  // this device's copy of the static scratch (ca_attention_noalloc)
   std::string scratch_error;  // why it is null
 
+  // Plans of the last two windows asked for (a model that alternates windowed
+  // and full layers over one cache keeps both).
+  PlanSlot plans[2];
+  uint64_t plan_clock = 0;
+
   // host export buffers
   ca::Tables exported;
 
@@ -202,9 +232,12 @@ struct ca_cache {
     if (d_rowmap) (void)hipFree(d_rowmap);
     if (d_pf_ws) (void)hipFree(d_pf_ws);
     if (d_pf_cnt) (void)hipFree(d_pf_cnt);
+    for (PlanSlot& p : plans)
+      if (p.d) (void)hipFree(p.d);
   }
 
-  size_t esize() const { return cfg.dtype == CA_FP16 ? 2 : 4; }
+  bool kv4() const { return cfg.dtype == CA_FP16_KV4; }
+  size_t esize() const { return cfg.dtype == CA_FP32 ? 4 : 2; }  // of q and o
   int32_t token_head_bytes() const { return static_cast<int32_t>(2 * cfg.head_dim * esize()); }
 
   // Work lists for the current tree. Decode growth (new private chunks at
@@ -213,6 +246,26 @@ struct ca_cache {
   // tables and the work lists. `tables` keeps row_seq valid either way.
   void ensure_work() {
     if (work_valid && !tree.dirty()) return;
+    // The plans go along with the tree: decode growth is patched into them,
+    // after anything else they are made anew when next asked for.
+    if (tree.dirty())
+      for (PlanSlot& p : plans)
+        if (p.valid) {
+          p.valid = tree.private_growth_only() && ca::patch_plan(tree, work.row_of_seq, &p.plan);
+          p.uploaded = false;
+        }
+    if (kv4()) {  // its calls run over plans: row order only
+      if (!work_valid || !tree.private_growth_only()) {
+        ca::build_tables(tree, &tables);
+        work = ca::WorkLists();
+        for (size_t r = 0; r < tables.row_seq.size(); ++r)
+          work.row_of_seq[tables.row_seq[r]] = static_cast<int32_t>(r);
+      }
+      work_valid = true;
+      dw_valid = false;
+      tree.clear_dirty();
+      return;
+    }
     bool patched = false;
     if (work_valid && tree.private_growth_only() && split_chunks <= 0 && !patch_error.size())
       patched = ca::patch_work(tree, &work);
@@ -329,6 +382,51 @@ struct ca_cache {
     return CA_OK;
   }
 
+  // The plan of a window for the current tree (host part).
+  PlanSlot& ensure_plan(int32_t window, int32_t sinks) {
+    ensure_work();
+    PlanSlot* at = nullptr;
+    for (PlanSlot& p : plans)
+      if (p.used && p.plan.window == window && p.plan.sinks == sinks) at = &p;
+    if (!at) {
+      at = plans[0].used <= plans[1].used ? &plans[0] : &plans[1];
+      at->valid = false;
+    }
+    at->used = ++plan_clock;
+    if (!at->valid) {
+      ca::build_tables(tree, &tables);
+      at->uploaded = false;
+      ca::build_plan(tree, tables, window, sinks, cfg.num_heads, num_cus, &at->plan);
+      at->valid = true;
+    }
+    return *at;
+  }
+
+  size_t plan_ws_bytes(const ca::Plan& p) const {
+    const size_t np = static_cast<size_t>(p.n_parts), H = cfg.num_heads, D = cfg.head_dim;
+    return align_up(np * H * D * 4, 256) + align_up(np * H * 2 * 4, 256);
+  }
+
+  ca_status upload_plan(PlanSlot* p, hipStream_t stream) {
+    const ca::Plan& P = p->plan;
+    const size_t bi = P.items.size() * sizeof(ca::PlanItem), bc = P.chunks.size() * sizeof(ca::PlanChunk),
+                 br = P.rows.size() * sizeof(ca::PlanRow);
+    p->o_chunks = align_up(bi, 16);
+    p->o_rows = p->o_chunks + align_up(bc, 16);
+    const size_t total = p->o_rows + br;
+    ca_status st = ensure_device(&p->d, &p->cap, total, stream, "plan alloc");
+    if (st != CA_OK) return st;
+    char* h = nullptr;
+    if ((st = p->stage.acquire(total, &h)) != CA_OK) return st;
+    std::memcpy(h, P.items.data(), bi);
+    std::memcpy(h + p->o_chunks, P.chunks.data(), bc);
+    std::memcpy(h + p->o_rows, P.rows.data(), br);
+    if ((st = p->stage.copy(p->d, total, stream)) != CA_OK) return st;
+    p->uploaded = true;
+    ++uploads;
+    return CA_OK;
+  }
+
   // Tree row -> caller row for a caller order given as seq_ids[0..n) (every
   // live sequence once); uploaded only when it differs from the device copy.
   ca_status upload_row_map(const int64_t* seq_ids, int64_t n, hipStream_t stream) {
@@ -403,10 +501,14 @@ struct ca_cache {
     std::unordered_set<int32_t> touched;
     auto flush = [&]() -> ca_status {
       if (batch.empty()) return CA_OK;
-      hipError_t e = ca::launch_kv_jobs(batch.data(), static_cast<int>(batch.size()),
-                                        cfg.dtype == CA_FP16 ? 0 : 1, cfg.num_heads, cfg.head_dim,
-                                        cfg.chunk_size, cfg.slot_stride, cfg.head_stride, k, v,
-                                        cfg.k_pool, cfg.v_pool, d_slot_len, stream);
+      hipError_t e =
+          kv4() ? ca::launch_kv4_jobs(batch.data(), static_cast<int>(batch.size()), cfg.num_heads,
+                                      cfg.head_dim, cfg.chunk_size, cfg.slot_stride, cfg.head_stride,
+                                      k, v, cfg.k_pool, cfg.v_pool, d_slot_len, stream)
+                : ca::launch_kv_jobs(batch.data(), static_cast<int>(batch.size()),
+                                     cfg.dtype == CA_FP16 ? 0 : 1, cfg.num_heads, cfg.head_dim,
+                                     cfg.chunk_size, cfg.slot_stride, cfg.head_stride, k, v,
+                                     cfg.k_pool, cfg.v_pool, d_slot_len, stream);
       batch.clear();
       touched.clear();
       if (e != hipSuccess) return hip_fail(e, "kv copy launch");
@@ -442,7 +544,7 @@ ca_status ca_create(const ca_config* cfg, ca_cache** out) try {
     int32_t dt;
     static_assert(sizeof(cfg->dtype) == sizeof(dt), "ca_dtype is a 32-bit enumeration");
     std::memcpy(&dt, &cfg->dtype, sizeof dt);
-    if (dt != CA_FP16 && dt != CA_FP32) return fail(CA_ERR_INVALID, "ca_create: bad dtype");
+    if (dt != CA_FP16 && dt != CA_FP32 && dt != CA_FP16_KV4) return fail(CA_ERR_INVALID, "ca_create: bad dtype");
   }
   if (cfg->num_slots < 1 || cfg->num_slots > INT32_MAX)
     return fail(CA_ERR_INVALID, "ca_create: num_slots out of range");
@@ -452,8 +554,10 @@ ca_status ca_create(const ca_config* cfg, ca_cache** out) try {
     return fail(CA_ERR_INVALID, "ca_create: pools must be 16-byte aligned");
   ca_config norm = *cfg;
   {
-    const int64_t tile = static_cast<int64_t>(cfg->chunk_size) * cfg->head_dim;
-    const int64_t es = cfg->dtype == CA_FP16 ? 2 : 4;
+    const bool kv4 = cfg->dtype == CA_FP16_KV4;
+    const int64_t tile = kv4 ? ca::kv4_tile_bytes(cfg->chunk_size, cfg->head_dim)
+                             : static_cast<int64_t>(cfg->chunk_size) * cfg->head_dim;
+    const int64_t es = kv4 ? 1 : cfg->dtype == CA_FP16 ? 2 : 4;
     if (norm.head_stride == 0) norm.head_stride = tile;
     if (norm.slot_stride == 0) norm.slot_stride = cfg->num_heads * norm.head_stride;
     if (norm.head_stride < tile || norm.slot_stride < (cfg->num_heads - 1) * norm.head_stride + tile)
@@ -610,6 +714,7 @@ ca_status ca_seq_order(const ca_cache* cache, int64_t* seq_ids, int64_t cap) try
 ca_status ca_workspace_size(const ca_cache* cache, size_t* bytes) try {
   if (!cache || !bytes) return fail(CA_ERR_INVALID, "ca_workspace_size: null argument");
   ca_cache* c = const_cast<ca_cache*>(cache);
+  if (c->kv4()) return ca_window_workspace_size(cache, ca::kNoWindow, 0, bytes);
   c->ensure_work();
   *bytes = c->ws_bytes();
   return CA_OK;
@@ -665,6 +770,90 @@ static ca_status launch_attention_call(ca_cache* cache, const void* q, void* o, 
   return CA_OK;
 }
 
+// Enqueue a decode call over an uploaded plan.
+static ca_status launch_plan_call(ca_cache* cache, const PlanSlot& slot, const void* q, void* o,
+                                  float scale, char* ws, int32_t* cnt, const int32_t* row_map,
+                                  hipStream_t s) {
+  const float sc = scale == 0.f ? 1.f / std::sqrt(static_cast<float>(cache->cfg.head_dim)) : scale;
+  ca::PlanArgs a{};
+  a.store = cache->kv4() ? ca::kStoreKv4 : cache->cfg.dtype == CA_FP16 ? ca::kStoreF16 : ca::kStoreF32;
+  a.H = cache->cfg.num_heads;
+  a.D = cache->cfg.head_dim;
+  a.C = cache->cfg.chunk_size;
+  a.q = q;
+  a.o = o;
+  a.kpool = cache->cfg.k_pool;
+  a.vpool = cache->cfg.v_pool;
+  a.ss = cache->cfg.slot_stride;
+  a.hs = cache->cfg.head_stride;
+  a.slot_len = cache->d_slot_len;
+  a.items = reinterpret_cast<const ca::PlanItem*>(slot.d);
+  a.chunks = reinterpret_cast<const ca::PlanChunk*>(slot.d + slot.o_chunks);
+  a.rows = reinterpret_cast<const ca::PlanRow*>(slot.d + slot.o_rows);
+  a.n_items = static_cast<int>(slot.plan.items.size());
+  a.chunk_stride = slot.plan.stride;
+  a.window = slot.plan.window;
+  a.sinks = slot.plan.sinks;
+  const size_t np = static_cast<size_t>(slot.plan.n_parts);
+  const size_t o_bytes = np * a.H * a.D * 4;
+  if (o_bytes > 0xFFFFFFFFull || static_cast<uint64_t>(a.n_items) * a.H > 0x7fffffffull)
+    return fail(CA_ERR_INVALID, "ca_attention: the call has more partials or blocks than one launch takes");
+  a.ws_o = reinterpret_cast<float*>(ws);
+  a.ws_o_bytes = static_cast<uint32_t>(o_bytes);
+  a.ws_ml = np ? reinterpret_cast<float*>(ws + align_up(o_bytes, 256)) : nullptr;
+  a.qscale = sc * 1.4426950408889634f;
+  a.cnt = cnt;
+  a.cnt_layout = ca::counter_layout(static_cast<size_t>(cache->tree.num_seqs()), a.H);
+  a.row_map = row_map;
+  const hipError_t e = ca::launch_plan_attention(a, s);
+  if (e != hipSuccess) return hip_fail(e, "ca_attention launch");
+  return CA_OK;
+}
+
+// Window and sinks of a call as a plan holds them.
+static ca_status check_window(int64_t window, int64_t sinks, const char* what, int32_t* w, int32_t* k) {
+  if (window < 1) return fail(CA_ERR_INVALID, std::string(what) + ": window < 1");
+  if (sinks < 0) return fail(CA_ERR_INVALID, std::string(what) + ": sinks < 0");
+  *w = static_cast<int32_t>(std::min<int64_t>(window, ca::kNoWindow));
+  *k = static_cast<int32_t>(std::min<int64_t>(sinks, ca::kNoWindow));
+  return CA_OK;
+}
+
+// Positions of a plan are 30-bit.
+static ca_status check_lengths(const ca_cache* cache, const char* what) {
+  for (const auto& kv : cache->tree.seqs())
+    if (kv.second.length >= ca::kOpenEnd)
+      return fail(CA_ERR_INVALID, std::string(what) + ": sequence too long");
+  return CA_OK;
+}
+
+static ca_status plan_attention_impl(ca_cache* cache, const void* q, void* o, const int64_t* seq_ids,
+                                     int64_t n, int32_t window, int32_t sinks, float scale, void* ws,
+                                     size_t ws_bytes, void* stream) {
+  ca_status st = check_attention_io(cache, q, o, scale);
+  if (st != CA_OK) return st;
+  if ((st = check_lengths(cache, "ca_attention")) != CA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  PlanSlot& slot = cache->ensure_plan(window, sinks);
+  const size_t need = cache->plan_ws_bytes(slot.plan);
+  if (need > 0 && (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) || ws_bytes < need))
+    return fail(CA_ERR_WORKSPACE, "ca_attention: workspace missing, misaligned or smaller than " +
+                                      std::to_string(need) + " bytes");
+  const size_t counters = ca::counter_entries(static_cast<size_t>(cache->tree.num_seqs()),
+                                              static_cast<size_t>(cache->cfg.num_heads));
+  if ((!slot.uploaded || counters > cache->d_cnt_cap) && capturing(s))
+    return fail(CA_ERR_INVALID, "ca_attention: kernel context not current, and a call that is being "
+                                "captured cannot bring it up to date (prepare, and make one call, before)");
+  if (!slot.uploaded && (st = cache->upload_plan(&slot, s)) != CA_OK) return st;
+  const int32_t* row_map = nullptr;
+  if (seq_ids) {
+    if ((st = cache->upload_row_map(seq_ids, n, s)) != CA_OK) return st;
+    row_map = cache->d_rowmap;
+  }
+  if ((st = ca_cache::ensure_counters(&cache->d_cnt, &cache->d_cnt_cap, counters, s)) != CA_OK) return st;
+  return launch_plan_call(cache, slot, q, o, scale, static_cast<char*>(ws), cache->d_cnt, row_map, s);
+}
+
 static ca_status attention_impl(ca_cache* cache, const void* q, void* o, float scale, void* ws,
                                 size_t ws_bytes, void* stream, const int64_t* seq_ids,
                                 int64_t n) {
@@ -673,6 +862,8 @@ static ca_status attention_impl(ca_cache* cache, const void* q, void* o, float s
   if (seq_ids && n != cache->tree.num_seqs())
     return fail(CA_ERR_INVALID, "ca_attention_ordered: n differs from the number of live sequences");
   if (cache->tree.num_seqs() == 0) return CA_OK;
+  if (cache->kv4())
+    return plan_attention_impl(cache, q, o, seq_ids, n, ca::kNoWindow, 0, scale, ws, ws_bytes, stream);
   ca_status st = check_attention_io(cache, q, o, scale);
   if (st != CA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -714,6 +905,55 @@ ca_status ca_attention_ordered(ca_cache* cache, const void* q, void* o, const in
   return on_exception("ca_attention_ordered");
 }
 
+ca_status ca_window_workspace_size(const ca_cache* cache, int64_t window, int64_t sinks,
+                                   size_t* bytes) try {
+  if (!cache || !bytes) return fail(CA_ERR_INVALID, "ca_window_workspace_size: null argument");
+  int32_t w = 0, k = 0;
+  ca_status st = check_window(window, sinks, "ca_window_workspace_size", &w, &k);
+  if (st != CA_OK || (st = check_lengths(cache, "ca_window_workspace_size")) != CA_OK) return st;
+  ca_cache* c = const_cast<ca_cache*>(cache);
+  *bytes = c->plan_ws_bytes(c->ensure_plan(w, k).plan);
+  return CA_OK;
+} catch (...) {
+  return on_exception("ca_window_workspace_size");
+}
+
+ca_status ca_prepare_window(ca_cache* cache, int64_t window, int64_t sinks, void* stream,
+                            int32_t* uploaded) try {
+  if (uploaded) *uploaded = 0;
+  if (!cache) return fail(CA_ERR_INVALID, "ca_prepare_window: null cache");
+  int32_t w = 0, k = 0;
+  ca_status st = check_window(window, sinks, "ca_prepare_window", &w, &k);
+  if (st != CA_OK || (st = check_lengths(cache, "ca_prepare_window")) != CA_OK) return st;
+  PlanSlot& slot = cache->ensure_plan(w, k);
+  if (cache->table_only || cache->tree.num_seqs() == 0 || slot.uploaded) return CA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (capturing(s))
+    return fail(CA_ERR_INVALID, "ca_prepare_window: the context cannot be uploaded by a call that is "
+                                "being captured");
+  if ((st = cache->upload_plan(&slot, s)) != CA_OK) return st;
+  if (uploaded) *uploaded = 1;
+  return CA_OK;
+} catch (...) {
+  return on_exception("ca_prepare_window");
+}
+
+ca_status ca_attention_window(ca_cache* cache, const void* q, void* o, const int64_t* seq_ids, int64_t n,
+                              int64_t window, int64_t sinks, float scale, void* ws, size_t ws_bytes,
+                              void* stream) try {
+  if (!cache) return fail(CA_ERR_INVALID, "ca_attention_window: null cache");
+  if (cache->table_only) return fail(CA_ERR_INVALID, "ca_attention_window: table-only cache");
+  int32_t w = 0, k = 0;
+  ca_status st = check_window(window, sinks, "ca_attention_window", &w, &k);
+  if (st != CA_OK) return st;
+  if (seq_ids && n != cache->tree.num_seqs())
+    return fail(CA_ERR_INVALID, "ca_attention_window: n differs from the number of live sequences");
+  if (cache->tree.num_seqs() == 0) return CA_OK;
+  return plan_attention_impl(cache, q, o, seq_ids, n, w, k, scale, ws, ws_bytes, stream);
+} catch (...) {
+  return on_exception("ca_attention_window");
+}
+
 ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float scale,
                                void* stream) try {
   if (!cache) return fail(CA_ERR_INVALID, "ca_attention_noalloc: null cache");
@@ -724,17 +964,21 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
   // Everything the call needs must exist already: the kernel context on the
   // device (ca_prepare or an earlier attention call after the last tree or
   // tuning change) and, for the two-stream schedule, its stream.
-  if (!cache->work_valid || cache->tree.dirty() || !cache->dw_valid)
+  PlanSlot* plan = nullptr;  // a 4-bit cache's context
+  if (cache->kv4())
+    for (PlanSlot& p : cache->plans)
+      if (p.used && p.plan.window == ca::kNoWindow && p.valid && p.uploaded) plan = &p;
+  if (!cache->work_valid || cache->tree.dirty() || !(cache->kv4() ? plan != nullptr : cache->dw_valid))
     return fail(CA_ERR_INVALID,
                 "ca_attention_noalloc: kernel context not current (call ca_prepare after the "
                 "last tree or tuning change)");
-  if (cache->schedule == 3 && !cache->side.stream)
+  if (!plan && cache->schedule == 3 && !cache->side.stream)
     return fail(CA_ERR_INVALID, "ca_attention_noalloc: the two-stream schedule's stream does not "
                                 "exist yet (one ca_attention call creates it)");
   if (!cache->scratch)
     return fail(CA_ERR_DEVICE, "ca_attention_noalloc: no device scratch: " + cache->scratch_error);
   const size_t counters = static_cast<size_t>(cache->tree.num_seqs()) * cache->cfg.num_heads;
-  const size_t parts = cache->ws_bytes();
+  const size_t parts = plan ? cache->plan_ws_bytes(plan->plan) : cache->ws_bytes();
   if (counters * sizeof(int32_t) > ca::kScratchCounterBytes ||
       parts > ca::kScratchBytes - ca::kScratchCounterBytes)
     return fail(CA_ERR_WORKSPACE,
@@ -754,6 +998,9 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
                                                static_cast<size_t>(cache->cfg.num_heads))),
       0, s);
   if (e != hipSuccess) return hip_fail(e, "ca_attention_noalloc counter clear");
+  if (plan)
+    return launch_plan_call(cache, *plan, q, o, scale, cache->scratch + ca::kScratchCounterBytes, cnt,
+                            nullptr, s);
   return launch_attention_call(cache, q, o, scale, cache->scratch + ca::kScratchCounterBytes, cnt,
                                nullptr, s);
 } catch (...) {
@@ -763,6 +1010,7 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
 ca_status ca_prepare(ca_cache* cache, void* stream, int32_t* uploaded) try {
   if (uploaded) *uploaded = 0;
   if (!cache) return fail(CA_ERR_INVALID, "ca_prepare: null cache");
+  if (cache->kv4()) return ca_prepare_window(cache, ca::kNoWindow, 0, stream, uploaded);
   cache->ensure_work();
   if (cache->table_only || cache->tree.num_seqs() == 0 || cache->dw_valid) return CA_OK;
   ca_status st = cache->upload(static_cast<hipStream_t>(stream));

@@ -5,6 +5,7 @@
 
 #include <cstdint>
 
+#include "plan.hpp"
 #include "tree.hpp"
 #include "worklist.hpp"
 
@@ -141,5 +142,42 @@ constexpr int kKvJobsPerLaunch = 64;
 hipError_t launch_kv_jobs(const KvJob* jobs, int n, int dtype, int H, int D, int C, int64_t ss,
                           int64_t hs, const void* k, const void* v, void* kpool, void* vpool,
                           int32_t* slot_len, hipStream_t stream);
+
+// The same for a cache held in 4 bits (kv4.hip); strides in bytes, k and v
+// fp16 rows.
+hipError_t launch_kv4_jobs(const KvJob* jobs, int n, int H, int D, int C, int64_t ss, int64_t hs,
+                           const void* k, const void* v, void* kpool, void* vpool, int32_t* slot_len,
+                           hipStream_t stream);
+
+// What a pool holds (the values of ca_dtype).
+enum Store : int { kStoreF16 = 0, kStoreF32 = 1, kStoreKv4 = 2 };
+
+// Decode attention over a plan (window.hip): a sliding window with sinks over
+// any pool, and every decode call over a 4-bit one.
+struct PlanArgs {
+  int store;  // Store
+  int H, D, C;
+  const void* q;
+  void* o;
+  const void* kpool;
+  const void* vpool;
+  int64_t ss, hs;  // pool strides of a slot and of a head (elements; bytes of a 4-bit pool)
+  const int32_t* slot_len;
+  const PlanItem* items;
+  const PlanChunk* chunks;  // [n_items][chunk_stride]
+  const PlanRow* rows;
+  int n_items;
+  int chunk_stride;
+  int window;  // positions a query sees besides the sinks (kNoWindow: all)
+  int sinks;
+  float* ws_o;   // [n_parts][H][D]
+  float* ws_ml;  // [n_parts][H][2] (running max in log2 units, sum)
+  uint32_t ws_o_bytes;
+  float qscale;  // softmax scale * log2(e)
+  int32_t* cnt;
+  int cnt_layout;
+  const int32_t* row_map = nullptr;
+};
+hipError_t launch_plan_attention(const PlanArgs& a, hipStream_t stream);
 
 }  // namespace ca

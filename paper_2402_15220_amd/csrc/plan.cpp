@@ -1,0 +1,134 @@
+// Decode plan of windowed calls and of 4-bit caches; see plan.hpp.
+#include "plan.hpp"
+
+#include <algorithm>
+
+namespace ca {
+
+void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t sinks, int32_t heads,
+                int32_t num_cus, Plan* out) {
+  Plan& P = *out;
+  const int32_t B = static_cast<int32_t>(t.row_seq.size());
+  const int32_t nn = static_cast<int32_t>(t.node_slot.size());
+  const int32_t C = tree.chunk_size();
+  P = Plan();
+  P.window = window;
+  P.sinks = sinks;
+
+  std::vector<int32_t> lo(B);  // first position of each row's window
+  for (int32_t r = 0; r < B; ++r) {
+    const int64_t len = tree.seqs().at(t.row_seq[r]).length;
+    lo[r] = static_cast<int32_t>(std::max<int64_t>(0, len - window));
+  }
+
+  // Runs in level order, so a run's parent comes before it.
+  struct Run {
+    int32_t row_begin, row_end, lo, parent, ord = 0;
+    std::vector<int32_t> seen;  // visible nodes, root -> leaf
+    int64_t tokens = 0;
+    int32_t pieces = 0;
+  };
+  std::vector<Run> runs;
+  std::vector<int32_t> run_of(nn);
+  for (int32_t i = 0; i < nn; ++i) {
+    const int32_t p = t.node_parent[i], rb = t.node_row_begin[i], re = t.node_row_end[i];
+    if (p >= 0 && t.node_row_begin[p] == rb && t.node_row_end[p] == re) {
+      run_of[i] = run_of[p];
+    } else {
+      run_of[i] = static_cast<int32_t>(runs.size());
+      Run r;
+      r.row_begin = rb;
+      r.row_end = re;
+      r.lo = *std::min_element(lo.begin() + rb, lo.begin() + re);
+      r.parent = p < 0 ? -1 : run_of[p];
+      runs.push_back(std::move(r));
+    }
+    Run& r = runs[run_of[i]];
+    const int32_t start = t.node_start_pos[i], end = start + t.node_len[i];
+    if (start < sinks || end > r.lo) {
+      r.seen.push_back(i);
+      // tokens read: the part in the window and the sinks
+      r.tokens += end - std::max(start, std::min(end, r.lo)) +
+                  std::max(0, std::min({end, sinks, std::max(start, r.lo)}) - start);
+    }
+  }
+
+  // Pieces: about four blocks a compute unit, of at least 128 tokens (one
+  // step of a block's four wavefronts).
+  int64_t load = 0;
+  for (const Run& r : runs)
+    load += (r.row_end - r.row_begin + kPlanRows - 1) / kPlanRows * r.tokens * heads;
+  const int64_t piece_tokens = std::max<int64_t>(128, (load + 4 * num_cus - 1) / (4 * num_cus));
+  P.piece_chunks = static_cast<int32_t>(std::min<int64_t>(kPlanChunks - 2, std::max<int64_t>(1, (piece_tokens + C - 1) / C)));
+  int32_t longest = 0;
+  for (Run& r : runs) {
+    const int32_t n = static_cast<int32_t>(r.seen.size());
+    r.pieces = (n + P.piece_chunks - 1) / P.piece_chunks;
+    if (r.parent >= 0) r.ord = runs[r.parent].ord + runs[r.parent].pieces;
+    if (r.pieces) longest = std::max(longest, (n + r.pieces - 1) / r.pieces);
+  }
+  P.stride = longest + 2;  // room for growth
+
+  P.rows.resize(B);
+  P.last_item.assign(B, -1);
+  for (int32_t r = 0; r < B; ++r) {
+    const int32_t leaf = t.path_node[t.path_ptr[r + 1] - 1];
+    const Run& run = runs[run_of[leaf]];
+    const int32_t np = run.ord + run.pieces;
+    P.rows[r] = {t.node_slot[leaf], t.node_start_pos[leaf], np > 1 ? P.n_parts : -1, np};
+    if (np > 1) P.n_parts += np;
+  }
+
+  // Shared runs first: their blocks work on up to 16 rows each.
+  for (int pass = 0; pass < 2; ++pass) {
+    for (const Run& r : runs) {
+      const bool shared = r.row_end - r.row_begin > 1;
+      if (shared != (pass == 0)) continue;
+      const int32_t n = static_cast<int32_t>(r.seen.size());
+      for (int32_t k = 0; k < r.pieces; ++k) {
+        const int32_t c0 = static_cast<int32_t>(static_cast<int64_t>(n) * k / r.pieces);
+        const int32_t c1 = static_cast<int32_t>(static_cast<int64_t>(n) * (k + 1) / r.pieces);
+        for (int32_t rb = r.row_begin; rb < r.row_end; rb += kPlanRows) {
+          const size_t at = P.chunks.size();
+          P.chunks.resize(at + P.stride, PlanChunk{0, 0, 0, 0});
+          for (int32_t c = c0; c < c1; ++c) {
+            const int32_t i = r.seen[c], start = t.node_start_pos[i];
+            const bool open = !shared && c == n - 1;
+            P.chunks[at + c - c0] = {t.node_slot[i], start, open ? kOpenEnd : start + t.node_len[i], 0};
+          }
+          if (!shared && c1 == n) P.last_item[rb] = static_cast<int32_t>(P.items.size());
+          const int32_t re = std::min(rb + kPlanRows, r.row_end);
+          const int32_t ilo = *std::min_element(lo.begin() + rb, lo.begin() + re);
+          P.items.push_back({rb, re - rb, c1 - c0, r.ord + k, ilo, {0, 0, 0}});
+        }
+      }
+    }
+  }
+}
+
+bool patch_plan(const ChunkTree& tree, const std::unordered_map<int64_t, int32_t>& row_of_seq, Plan* p) {
+  std::vector<int32_t> added(p->items.size(), 0);
+  for (const auto& g : tree.grown()) {
+    const auto it = row_of_seq.find(g.first);
+    if (it == row_of_seq.end() || p->last_item[it->second] < 0) return false;
+    const int32_t i = p->last_item[it->second];
+    if (p->items[i].n_chunks + ++added[i] > p->stride) return false;
+  }
+  for (const auto& g : tree.grown()) {
+    const int32_t row = row_of_seq.at(g.first), i = p->last_item[row];
+    PlanRow& r = p->rows[row];
+    PlanItem& item = p->items[i];
+    PlanChunk* c = p->chunks.data() + static_cast<size_t>(i) * p->stride;
+    const Node& nd = tree.node(g.second);
+    // the chunk that was last is full now
+    const int32_t start = r.last_start + static_cast<int32_t>(tree.node(nd.parent).tokens.size());
+    c[item.n_chunks - 1].end = start;
+    c[item.n_chunks] = {nd.slot, start, kOpenEnd, 0};
+    ++item.n_chunks;
+    r.last_slot = nd.slot;
+    r.last_start = start;
+  }
+  return true;
+}
+
+}  // namespace ca
