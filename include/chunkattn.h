@@ -313,7 +313,7 @@ ca_status ca_prepare(ca_cache* cache, void* stream, int32_t* uploaded);
  *   q      device [n_q][H][d], 16-byte aligned; o the same shape, written
  *   n_q    0 <= n_q <= L (0 is a no-op); typically L - matched
  *   scale  softmax scale applied to q.k; 0 means 1/sqrt(d)
- * fp16 caches only. Enqueue on the stream of the insert/extend that wrote
+ * fp16 and 4-bit caches only. Enqueue on the stream of the insert/extend that wrote
  * the K/V rows. The path (chunk slots and start positions, 8 bytes per
  * chunk) travels inside the kernel arguments for up to 255 chunks; a longer
  * one is copied to the device through library-owned pinned staging.
@@ -330,6 +330,19 @@ ca_status ca_prepare(ca_cache* cache, void* stream, int32_t* uploaded);
  * n_q > L), NOT_FOUND, DEVICE. */
 ca_status ca_prefill_attention(ca_cache* cache, int64_t seq_id, const void* q, void* o,
                                int64_t n_q, float scale, void* stream);
+
+/* Prefill attention with a sliding window and sinks: as ca_prefill_attention,
+ * but the query at position p sees the positions j <= p with j < sinks or
+ * j > p - window (window >= 1, sinks >= 0; ca_attention_window's rule for
+ * each query). Chunks that no query of the call sees are not read, and values
+ * that a query does not see, NaN and infinite ones among them, do not reach
+ * its o; where it sees a V element that is not finite its o is not finite
+ * there. fp16 and 4-bit caches; a 4-bit cache's values are taken as fp16,
+ * low + scale * code with one rounding. A call being captured is refused
+ * (INVALID) where more than 255 chunks are seen or the library's partials
+ * would have to grow. Errors as ca_prefill_attention. */
+ca_status ca_prefill_window(ca_cache* cache, int64_t seq_id, const void* q, void* o, int64_t n_q,
+                            int64_t window, int64_t sinks, float scale, void* stream);
 
 /* Host views of the canonical tables for the current tree (see ca_tables).
  * Lengths reflect every call made so far. */

@@ -36,7 +36,8 @@ CA_FP16_KV4 = 2
 EXPORTED = ["ca_create", "ca_destroy", "ca_match", "ca_insert", "ca_extend", "ca_append_batch",
             "ca_remove", "ca_num_seqs", "ca_seq_order", "ca_workspace_size", "ca_attention",
             "ca_attention_ordered", "ca_attention_noalloc", "ca_attention_window",
-            "ca_window_workspace_size", "ca_prepare_window", "ca_prefill_attention", "ca_prepare",
+            "ca_window_workspace_size", "ca_prepare_window", "ca_prefill_attention", "ca_prefill_window",
+            "ca_prepare",
             "ca_export_tables", "ca_stats", "ca_set_tuning", "ca_last_error"]
 
 
@@ -93,6 +94,7 @@ def load():
         "ca_workspace_size": [vp, ctypes.POINTER(ctypes.c_size_t)],
         "ca_attention": [vp, vp, vp, ctypes.c_float, vp, ctypes.c_size_t, vp],
         "ca_prefill_attention": [vp, i64, vp, vp, i64, ctypes.c_float, vp],
+        "ca_prefill_window": [vp, i64, vp, vp, i64, i64, i64, ctypes.c_float, vp],
         "ca_prepare": [vp, vp, ctypes.POINTER(i32)],
         "ca_attention_ordered": [vp, vp, vp, _P64, i64, ctypes.c_float, vp, ctypes.c_size_t, vp],
         "ca_attention_noalloc": [vp, vp, vp, ctypes.c_float, vp],
@@ -244,6 +246,10 @@ def ca_prepare(h, stream=None) -> bool:
 
 def ca_prefill_attention(h, seq_id, q, o, n_q, scale, stream=None):
     _check(load().ca_prefill_attention(h, seq_id, q, o, n_q, ctypes.c_float(scale), stream))
+
+
+def ca_prefill_window(h, seq_id, q, o, n_q, window, sinks, scale, stream=None):
+    _check(load().ca_prefill_window(h, seq_id, q, o, n_q, window, sinks, ctypes.c_float(scale), stream))
 
 
 def ca_export_tables(h) -> dict:

@@ -208,9 +208,11 @@ class Cache:
         B.ca_attention_noalloc(self.h, q.data_ptr(), out.data_ptr(), scale, self.stream())
         return out
 
-    def prefill(self, seq_id, q, out=None, scale: float = 0.0):
+    def prefill(self, seq_id, q, out=None, scale: float = 0.0, window: int | None = None, sinks: int = 0):
         """Causal attention of sequence ``seq_id``'s last q.shape[0] tokens over
-        its whole K/V (prefill after a prefix-matched insert). q: [n_q, H, d]."""
+        its whole K/V (prefill after a prefix-matched insert). q: [n_q, H, d].
+        ``window``: each query sees the ``window`` positions up to its own and
+        the first ``sinks``; without it, all up to its own."""
         if self.table_only:
             raise ValueError("table-only cache has no attention")
         if not isinstance(q, torch.Tensor) or q.dim() != 3:
@@ -219,6 +221,10 @@ class Cache:
         if out is None:
             out = torch.empty_like(q)
         self._check_rows(out, q.shape[0], "out")
+        if self._window(window, sinks):
+            B.ca_prefill_window(self.h, seq_id, q.data_ptr(), out.data_ptr(), q.shape[0], window, sinks,
+                                scale, self.stream())
+            return out
         B.ca_prefill_attention(self.h, seq_id, q.data_ptr(), out.data_ptr(), q.shape[0], scale,
                                self.stream())
         return out

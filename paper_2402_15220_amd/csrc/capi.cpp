@@ -1021,10 +1021,131 @@ ca_status ca_prepare(ca_cache* cache, void* stream, int32_t* uploaded) try {
   return on_exception("ca_prepare");
 }
 
+// Prefill over the 16-row tiles of a path (window_prefill.hip): what a query
+// sees may be a window, and the pool fp16 or 4-bit.
+static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void* q, void* o, int64_t n_q,
+                                     int32_t window, int32_t sinks, float scale, void* stream,
+                                     const char* what) {
+  if (cache->table_only) return fail(CA_ERR_INVALID, std::string(what) + ": table-only cache");
+  if (cache->cfg.dtype == CA_FP32) return fail(CA_ERR_INVALID, std::string(what) + ": not for fp32 caches");
+  const auto& seqs = cache->tree.seqs();
+  auto it = seqs.find(seq_id);
+  if (it == seqs.end()) return fail(CA_ERR_NOT_FOUND, std::string(what) + ": unknown sequence");
+  const int64_t L = it->second.length;
+  if (n_q < 0 || n_q > L) return fail(CA_ERR_INVALID, std::string(what) + ": need 0 <= n_q <= length");
+  if (n_q == 0) return CA_OK;
+  ca_status st = check_attention_io(cache, q, o, scale);
+  if (st != CA_OK) return st;
+  if (L >= ca::kOpenEnd) return fail(CA_ERR_INVALID, std::string(what) + ": sequence too long");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+
+  // the chunks that some query sees, root -> leaf
+  std::vector<int32_t> path;
+  for (int32_t id = it->second.term; id != ca::ChunkTree::kRoot; id = cache->tree.node(id).parent)
+    path.push_back(id);
+  std::reverse(path.begin(), path.end());
+  const int64_t lo = std::max<int64_t>(0, L - n_q - window + 1);
+  std::vector<int32_t>& hp = cache->prefill_host_path;
+  hp.clear();
+  std::vector<int32_t> starts, ends;
+  int32_t pos = 0;
+  for (int32_t id : path) {
+    const ca::Node& nd = cache->tree.node(id);
+    const int32_t end = pos + static_cast<int32_t>(nd.tokens.size());
+    if (pos < sinks || end > lo) {
+      hp.push_back(nd.slot);
+      starts.push_back(pos);
+      ends.push_back(end);
+    }
+    pos = end;
+  }
+  if (pos != L) return fail(CA_ERR_INVALID, std::string(what) + ": inconsistent path");
+  const int32_t nc = static_cast<int32_t>(hp.size());
+  hp.insert(hp.end(), starts.begin(), starts.end());
+  hp.insert(hp.end(), ends.begin(), ends.end());
+
+  ca::WindowPrefillArgs a{};
+  a.store = cache->kv4() ? ca::kStoreKv4 : ca::kStoreF16;
+  a.H = cache->cfg.num_heads;
+  a.D = cache->cfg.head_dim;
+  a.C = cache->cfg.chunk_size;
+  a.q = q;
+  a.o = o;
+  a.kpool = cache->cfg.k_pool;
+  a.vpool = cache->cfg.v_pool;
+  a.ss = cache->cfg.slot_stride;
+  a.hs = cache->cfg.head_stride;
+  a.n_chunks = nc;
+  a.n_q = static_cast<int>(n_q);
+  a.L = static_cast<int>(L);
+  a.window = window;
+  a.sinks = sinks;
+  a.qscale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(a.D)) : scale) * 1.4426950408889634f;
+
+  // 128-query tiles where they give every compute unit a block, else 64-query
+  // ones, whose keys are cut into parts of at least four units while two
+  // blocks a compute unit are not there.
+  const int64_t cus = cache->num_cus;
+  a.tile_rows = (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
+  const int64_t tiles = (n_q + a.tile_rows - 1) / a.tile_rows * a.H;
+  const int64_t units = (std::min<int64_t>(L, std::min<int64_t>(L, window) + a.tile_rows) +
+                         std::min<int64_t>(L, sinks)) / 64;
+  if (a.tile_rows == 64)
+    a.n_split = static_cast<int>(std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>(2 * cus / tiles, units / 4))));
+  const size_t ws = a.n_split > 1 ? static_cast<size_t>(tiles) * a.n_split *
+                                        ca::window_prefill_part_bytes(a.tile_rows, a.D)
+                                  : 0;
+  const size_t counters = a.n_split > 1 ? static_cast<size_t>(tiles) << ca::tile_counter_shift(static_cast<size_t>(tiles)) : 0;
+  const size_t path_bytes = hp.size() * sizeof(int32_t);
+  const bool inline_path = nc <= ca::kPrefillInlineChunks;
+  if ((!inline_path || ws > cache->d_pf_ws_cap || counters > cache->d_pf_cnt_cap) && capturing(s))
+    return fail(CA_ERR_INVALID, std::string(what) + ": a call that is being captured can neither copy a "
+                                                    "long path nor grow the partials' memory");
+  if (inline_path) {
+    a.host_path = hp.data();
+  } else {
+    char* h = nullptr;
+    if ((st = cache->prefill_stage.acquire(path_bytes, &h)) != CA_OK) return st;
+    std::memcpy(h, hp.data(), path_bytes);
+    if ((st = ensure_device(&cache->d_path, &cache->d_path_cap, path_bytes, s, "prefill path")) != CA_OK)
+      return st;
+    if ((st = cache->prefill_stage.copy(cache->d_path, path_bytes, s)) != CA_OK) return st;
+    a.path = reinterpret_cast<const int32_t*>(cache->d_path);
+  }
+  if (a.n_split > 1) {
+    if ((st = ensure_device(reinterpret_cast<char**>(&cache->d_pf_ws), &cache->d_pf_ws_cap, ws, s,
+                            "prefill partials")) != CA_OK)
+      return st;
+    if ((st = ca_cache::ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap, counters, s)) != CA_OK)
+      return st;
+    a.ws = cache->d_pf_ws;
+    a.ws_bytes = ws;
+    a.cnt = cache->d_pf_cnt;
+    a.cnt_shift = ca::tile_counter_shift(static_cast<size_t>(tiles));
+  }
+  const hipError_t e = ca::launch_window_prefill(a, s);
+  if (e != hipSuccess) return hip_fail(e, "prefill launch");
+  return CA_OK;
+}
+
+ca_status ca_prefill_window(ca_cache* cache, int64_t seq_id, const void* q, void* o, int64_t n_q,
+                            int64_t window, int64_t sinks, float scale, void* stream) try {
+  if (!cache) return fail(CA_ERR_INVALID, "ca_prefill_window: null cache");
+  int32_t w = 0, k = 0;
+  const ca_status st = check_window(window, sinks, "ca_prefill_window", &w, &k);
+  if (st != CA_OK) return st;
+  return window_prefill_impl(cache, seq_id, q, o, n_q, w, k, scale, stream, "ca_prefill_window");
+} catch (...) {
+  return on_exception("ca_prefill_window");
+}
+
 ca_status ca_prefill_attention(ca_cache* cache, int64_t seq_id, const void* q, void* o,
                                int64_t n_q, float scale, void* stream) try {
   if (!cache) return fail(CA_ERR_INVALID, "ca_prefill_attention: null cache");
   if (cache->table_only) return fail(CA_ERR_INVALID, "ca_prefill_attention: table-only cache");
+  if (cache->kv4())
+    return window_prefill_impl(cache, seq_id, q, o, n_q, ca::kNoWindow, 0, scale, stream,
+                               "ca_prefill_attention");
   if (cache->cfg.dtype != CA_FP16)
     return fail(CA_ERR_INVALID, "ca_prefill_attention: fp16 caches only");
   const auto& seqs = cache->tree.seqs();
