@@ -48,53 +48,17 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // slack of the softmax reference maximum, in log2 units: P <= 2^kLazy, so
 // that most steps leave the accumulators alone
 constexpr float kLazy = 4.f;
-// 4-bit: the largest scale in use stands for 2^kScaleTop, so P s_v <= 2^15
-constexpr float kScaleTop = 2048.f;
+// 4-bit: the reference of the scales stands for 2^kScaleTop, so that
+// P s_v <= 2^(kScaleTop + kLazy) stays in fp16's range
+constexpr int kScaleTop = 11;
 
 template <int S>
-struct Traits;
-template <>
-struct Traits<kStoreF16> {
+struct Traits {
   using T = _Float16;
-  static constexpr int kTiles = 2;  // 16-token tiles of a step
 };
 template <>
 struct Traits<kStoreF32> {
   using T = float;
-  static constexpr int kTiles = 1;
-};
-template <>
-struct Traits<kStoreKv4> {
-  using T = _Float16;
-  static constexpr int kTiles = 2;
-};
-
-// What one step loads, per lane.
-template <int S, int D>
-struct Stage;
-template <int D>
-struct Stage<kStoreF16, D> {
-  half8 k[2][D / 32];
-  u32x4 v[D / 16];  // granules of the 32 x D block, row-major
-};
-template <int D>
-struct Stage<kStoreF32, D> {
-  floatx4 k[D / 16];
-  floatx4 v[4][D / 64];
-};
-template <int D>
-struct Stage<kStoreKv4, D> {
-  uint32_t k[2][D / 32];
-  uint32_t v[2][D / 32];
-  u32x4 kp[2], vp[2];  // (scale, low) of tokens 4g .. 4g + 3
-};
-
-// Where a step's tokens lie: wave-uniform.
-struct Place {
-  int slot[2];
-  int row[2];  // first row of the tile in its chunk
-  int pos[2];  // its position
-  int end[2];  // position after the chunk's last token; <= pos: no token
 };
 
 // A (scale, low) pair. (__builtin_bit_cast of a vector's element itself reads
@@ -104,6 +68,8 @@ __device__ __forceinline__ half2v param(const u32x4& v, int i) {
   return __builtin_bit_cast(half2v, w);
 }
 
+// The eight codes of a word as fp16 halves: code * 2^-24 for elements 0, 1, 4
+// and 5, code * 2^-20 for 2, 3, 6 and 7.
 __device__ __forceinline__ half8 unpack8(uint32_t w) {
   const uint32_t x = w >> 8;
   const u32x4 r = {w & 0x000f000fu, w & 0x00f000f0u, x & 0x000f000fu, x & 0x00f000f0u};
@@ -119,50 +85,381 @@ __device__ __forceinline__ bool any_nonfinite(half8 x) {
   return bad;
 }
 
-template <int S, int D>
-__global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
-  using T = typename Traits<S>::T;
-  constexpr int TP = Traits<S>::kTiles;
+// w to the nearest fp16 below in size, as a float: the rest, w - rtz(w), takes
+// the next 11 bits
+__device__ __forceinline__ float top11(float w) {
+  return __uint_as_float(__float_as_uint(w) & 0xffffe000u);
+}
+
+// Keeps a rarely taken branch a branch.
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
+// What a block works on, wave-uniform except where said.
+struct Work {
+  const char* kbase;  // the head's tiles
+  const char* vbase;
+  int64_t ssb;        // bytes of a slot
+  PlanChunk my;       // per lane: chunk `lane` of the item
+  int nch;            // chunks
+  int C, tpc;         // rows and 16-row tiles of a chunk
+  uint32_t magic;     // x / tpc = mul_hi(x, magic) for tpc > 1
+  int n_tiles;
+  int sinks, lo_item;
+  int len, lo;        // per lane: length and window start of the lane's row
+};
+struct Tile {
+  int slot, row, pos, end;  // end <= pos: no token
+};
+__device__ __forceinline__ Tile tile_at(const Work& W, int i) {  // uniform i
+  const bool in = i < W.n_tiles;
+  i = in ? i : 0;
+  const int c = W.tpc == 1 ? i : static_cast<int>(__umulhi(static_cast<unsigned>(i), W.magic));
+  const int r = (i - c * W.tpc) * 16;
+  Tile t;
+  t.slot = __builtin_amdgcn_readlane(W.my.slot, c);
+  t.row = r;
+  t.pos = __builtin_amdgcn_readlane(W.my.start, c) + r;
+  t.end = in ? __builtin_amdgcn_readlane(W.my.end, c) : 0;
+  return t;
+}
+// Nothing of the tile is seen, whatever the rows' present lengths.
+__device__ __forceinline__ bool tile_hidden(const Work& W, const Tile& t) {
+  const int last = min(t.end, t.pos + 16) - 1;
+  return last < t.pos || (t.pos >= W.sinks && last < W.lo_item);
+}
+
+// The state a wavefront leaves for the fold: m_run, the sum n and, written to
+// `out` [row][OS], the unnormalised O of each row.
+
+// One row over a 4-bit pool, a wavefront's share: steps of 64 tokens, four
+// 16-token tiles. Here q is the A operand (16 equal rows) and the K rows are
+// columns, so the score of tile t's token n is in every lane of column n and
+// lane (g, n) takes tile g's: each lane has one token's softmax, its
+// parameters come in one 4-byte load, and P goes through 256 bytes of LDS to
+// the lanes that need it as B operand, its rounded part in even columns, the
+// rest in odd ones, so P loses nothing to fp16.
+template <int D>
+__device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const _Float16* qrow, int wv, int lane,
+                                        char* plds, float* out, float* om, float* on) {
   constexpr int KS = D / 32, DT = D / 16;
-  constexpr int VS = D + 16;                   // V tile row stride in LDS (halves)
-  constexpr int OS = D + 4;                    // merge buffer row stride (floats)
-  constexpr int VB = S == kStoreF16 ? 4 * 32 * VS * 2 : 0;
-  constexpr int MB = 4 * kPlanRows * OS * 4;
-  constexpr int BIG = VB > MB ? VB : MB;
-  __shared__ __align__(16) char lds[BIG];
-  __shared__ float s_m[4][kPlanRows], s_n[4][kPlanRows];
-  __shared__ int s_last[kPlanRows];
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const int H = A.H, C = A.C;
-  const int h = static_cast<int>(blockIdx.x % static_cast<unsigned>(H));
-  const int ib = static_cast<int>(blockIdx.x / static_cast<unsigned>(H));
-  const PlanItem item = A.items[ib];
-  // the chunks, one a lane (chunk_stride <= 64)
-  const PlanChunk my = A.chunks[static_cast<size_t>(ib) * A.chunk_stride + min(lane, A.chunk_stride - 1)];
-  const int nr = item.n_rows, nch = item.n_chunks;
-  const PlanRow prow = A.rows[item.row_begin + min(n16, nr - 1)];
-  const int io = A.row_map ? A.row_map[item.row_begin + min(n16, nr - 1)] : item.row_begin + min(n16, nr - 1);
-  const int len = prow.last_start + A.slot_len[prow.last_slot];
-  const int lo = max(0, len - A.window);
-  const int sinks = A.sinks;
+  half8 qf[KS];
+  float amax = 0.f, sum = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qf[s] = *reinterpret_cast<const half8*>(qrow + KS * 8 * g + 8 * s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = static_cast<float>(qf[s][i]);
+      amax = fmaxf(amax, fabsf(x));
+      sum += x;
+    }
+  }
+  amax = rows4_max(amax);
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  // q times 2^e with |q| 2^e in [2^10, 2^11): the 2^-4 of every second pair
+  // and a small q stay in the normal range
+  const int e = amax > 0.f && amax < INFINITY ? 11 - __builtin_amdgcn_frexp_expf(amax) : 0;
+  const float up = __builtin_amdgcn_ldexpf(1.f, e);
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      qf[s][i] = static_cast<_Float16>(static_cast<float>(qf[s][i]) * ((i & 2) ? up * 0.0625f : up));
+  const float qk = __builtin_amdgcn_ldexpf(A.qscale, 24 - e);  // score = qk (s_k a + low_k ql)
+  const float ql = __builtin_amdgcn_ldexpf(sum, e - 24);
 
-  // q as the B operand of S^T; a lane past the rows repeats the last one.
-  // 4-bit: q times 2^-e with |q| 2^-e in [2^10, 2^11], so that neither the
-  // 2^-4 of the second code of a pair nor a small q leaves the normal range.
-  const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
-  half8 qf[S == kStoreF32 ? 1 : KS];
-  floatx4 qx[S == kStoreF32 ? D / 16 : 1];
-  float qk = 0.f, ql = 0.f;  // 4-bit: factors of s_k and low_k
-  if constexpr (S == kStoreF32) {
+  const int pb = kv4_rows(W.C) * (D / 2);
+  uint32_t kx[4][KS], vx[4][KS];
+  uint32_t kp = 0, vp = 0;
+  Tile tn[4];  // the step being loaded
+  auto fetch = [&](int st) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) tn[t] = tile_at(W, 4 * st + t);
+  };
+  auto mine = [&](int Tile::*f) {  // the lane's tile's value
+    const int a = g & 1 ? tn[1].*f : tn[0].*f, b = g & 1 ? tn[3].*f : tn[2].*f;
+    return g & 2 ? b : a;
+  };
+  auto load_words = [&](const char* at, uint32_t (&x)[KS]) {
+    if constexpr (D == 128) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[s] = a[s];
+    } else {
+      const u32x2 a = *reinterpret_cast<const u32x2*>(at);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[s] = a[s];
+    }
+  };
+  int pos_n = 0, end_n = 0;
+  int64_t par_n = 0;
+  auto load_k = [&]() {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      load_words(W.kbase + tn[t].slot * W.ssb + (tn[t].row + n16) * (D / 2) + g * (D / 8), kx[t]);
+    par_n = mine(&Tile::slot) * W.ssb + pb + (mine(&Tile::row) + n16) * 4;
+    kp = *reinterpret_cast<const uint32_t*>(W.kbase + par_n);
+    pos_n = mine(&Tile::pos) + n16;
+    end_n = mine(&Tile::end);
+  };
+  Tile tv[4];
+  auto load_v = [&](int64_t par) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      load_words(W.vbase + tv[t].slot * W.ssb + tv[t].row * (D / 2) + lane * (D / 8), vx[t]);
+    vp = *reinterpret_cast<const uint32_t*>(W.vbase + par);
+  };
+  auto next = [&](int st) {
+    const int steps = (W.n_tiles + 3) / 4;
+    for (; st < steps; st += 4) {
+      fetch(st);
+      if (!(tile_hidden(W, tn[0]) && tile_hidden(W, tn[1]) && tile_hidden(W, tn[2]) && tile_hidden(W, tn[3]))) break;
+    }
+    return st < steps ? st : -1;
+  };
+
+  // m: reference of the scores plus log2 of the scales' reference
+  float m_run = kNegBig, m_sc = kNegBig, n_run = 0.f, base = 0.f, s_ref = 0.f;
+  floatx4 acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  _Float16* pl = reinterpret_cast<_Float16*>(plds);  // [hi, lo][pair][group][8]
+  int st = next(wv);
+  if (st >= 0) {
+    load_k();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) tv[t] = tn[t];
+    load_v(par_n);
+  }
+  while (st >= 0) {
+    floatx4 a[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      a[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        a[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qf[s], unpack8(kx[t][s]), a[t], 0, 0, 0);
+    }
+    const float raw = g & 2 ? (g & 1 ? a[3][0] : a[2][0]) : (g & 1 ? a[1][0] : a[0][0]);
+    const half2v kq = __builtin_bit_cast(half2v, kp);
+    const int pos = pos_n, end = end_n;
+    st = next(st + 4);
+    if (st >= 0) load_k();
+    const bool on = pos < end && pos < W.len && (pos >= W.lo || pos < W.sinks);
+    float sc = qk * __builtin_fmaf(raw, static_cast<float>(kq[0]), static_cast<float>(kq[1]) * ql);
+    sc = on ? sc : -INFINITY;
+    const half2v vq = __builtin_bit_cast(half2v, vp);
+    const float sv = on ? static_cast<float>(vq[0]) : 0.f, lv = on ? static_cast<float>(vq[1]) : 0.f;
+    if (__any(sc > m_sc + kLazy || sv > s_ref)) {
+      rare();
+      const float mx = wave_max(sc), sx = wave_max(sv);
+      if (mx > m_sc + kLazy) m_sc = mx;
+      if (sx > s_ref) s_ref = 2.f * sx;
+      const float m_new = s_ref > 0.f ? m_sc + __builtin_amdgcn_logf(s_ref) - kScaleTop : m_sc;
+      const float al = fast_exp2(m_run - m_new);
+      n_run *= al;
+      base *= al;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] *= al;
+      m_run = m_new;
+    }
+    const float p = fast_exp2(sc - m_run);
+    n_run += p;
+    base = __builtin_fmaf(p, lv, base);
+    const float w = p * sv * ((n16 & 2) ? 0.0625f : 1.f);
+    const float hi = top11(w);
+    const int at = (((g >> 1) * 4 + (n16 >> 2)) * 8) + (g & 1) * 4 + (n16 & 3);
+    pl[at] = static_cast<_Float16>(hi);
+    pl[64 + at] = static_cast<_Float16>(w - hi);
+    compiler_fence();
+    half8 pf[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) pf[r] = *reinterpret_cast<const half8*>(pl + 64 * (n16 & 1) + (r * 4 + g) * 8);
+    compiler_fence();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const half8 x = unpack8(vx[2 * r][s]), y = unpack8(vx[2 * r + 1][s]);
+        const half8 even = __builtin_shufflevector(x, y, 0, 1, 2, 3, 8, 9, 10, 11);
+        const half8 odd = __builtin_shufflevector(x, y, 4, 5, 6, 7, 12, 13, 14, 15);
+        acc[2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pf[r], acc[2 * s], 0, 0, 0);
+        acc[2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pf[r], acc[2 * s + 1], 0, 0, 0);
+      }
+    if (st >= 0) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) tv[t] = tn[t];
+      load_v(par_n);
+    }
+  }
+  n_run = wave_sum(n_run);
+  base = wave_sum(base);
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    floatx4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(acc[d][i] + dpp<0xB1>(acc[d][i]), 16777216.f, base);
+    if (n16 == 0) *reinterpret_cast<floatx4*>(out + 16 * d + 4 * g) = o;
+  }
+  if (lane == 0) {
+    *om = m_run;
+    *on = n_run;
+  }
+}
+
+// One row over an fp16 or fp32 pool, a wavefront's share: a row of the pool is
+// read by LPR lanes, 16 bytes each, a load covers RPL rows (1 KB), a step NL
+// loads of K and of V. Each group of LPR lanes keeps the softmax state of the
+// rows it saw, with P in 32 bits; the groups are folded at the end.
+template <int S, int D>
+__device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, const typename Traits<S>::T* qrow, int wv,
+                                          int lane, float* out, float* om, float* on) {
+  using T = typename Traits<S>::T;
+  constexpr int E = 16 / sizeof(T);                 // elements of a lane
+  constexpr int LPR = D / E, RPL = 64 / LPR;
+  constexpr int NL = 8;                             // loads of a step
+  constexpr int TP = NL * RPL / 16;                 // its tiles
+  constexpr int LT = NL / TP;                       // loads of a tile
+  constexpr int RB = D * static_cast<int>(sizeof(T));
+  const int gi = lane / LPR, li = lane % LPR;
+  float qv[E];
+  Elem<T>::unpack(*reinterpret_cast<const uint4*>(qrow + E * li), qv);
+  uint4 kx[NL], vx[NL];
+  Tile tn[TP], tv[TP];
+  auto fetch = [&](int st) {
+#pragma unroll
+    for (int t = 0; t < TP; ++t) tn[t] = tile_at(W, TP * st + t);
+  };
+  auto load = [&](const char* base, const Tile (&t)[TP], uint4 (&x)[NL]) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const Tile& y = t[i / LT];
+      // rows past the chunk's size read its last one again
+      const int r = min(y.row + (i % LT) * RPL + gi, W.C - 1);
+      x[i] = *reinterpret_cast<const uint4*>(base + y.slot * W.ssb + static_cast<size_t>(r) * RB + 16 * li);
+    }
+  };
+  auto next = [&](int st) {
+    const int steps = (W.n_tiles + TP - 1) / TP;
+    for (; st < steps; st += 4) {
+      fetch(st);
+      bool hid = true;
+#pragma unroll
+      for (int t = 0; t < TP; ++t) hid &= tile_hidden(W, tn[t]);
+      if (!hid) break;
+    }
+    return st < steps ? st : -1;
+  };
+  float m = kNegBig, n = 0.f;
+  float acc[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc[j] = 0.f;
+  int st = next(wv);
+  if (st >= 0) {
+    load(W.kbase, tn, kx);
+    load(W.vbase, tn, vx);
+  }
+  while (st >= 0) {
+#pragma unroll
+    for (int t = 0; t < TP; ++t) tv[t] = tn[t];
+    float sc[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      float x[E], d = 0.f;
+      Elem<T>::unpack(kx[i], x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) d = __builtin_fmaf(x[j], qv[j], d);
+      sc[i] = group_sum<LPR>(d) * A.qscale;
+    }
+    st = next(st + 4);
+    if (st >= 0) load(W.kbase, tn, kx);
+    bool all = true;
+#pragma unroll
+    for (int t = 0; t < TP; ++t) {
+      const int last = tv[t].pos + 16;
+      all &= last <= tv[t].end && last <= W.len && (tv[t].pos >= W.lo || last <= W.sinks);
+    }
+    if (!__builtin_amdgcn_readfirstlane(all)) {
+      rare();
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int j = tv[i / LT].pos + (i % LT) * RPL + gi;
+        const bool on = j < tv[i / LT].end && j < W.len && (j >= W.lo || j < W.sinks);
+        sc[i] = on ? sc[i] : -INFINITY;
+        if (!on) vx[i] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int i = 1; i < NL; ++i) mx = fmaxf(mx, sc[i]);
+    const float mn = mx > m + kLazy ? mx : m;
+    if (__any(mn != m)) {
+      rare();
+      const float al = fast_exp2(m - mn);
+      n *= al;
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc[j] *= al;
+      m = mn;
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const float p = fast_exp2(sc[i] - m);
+      n += p;
+      float x[E];
+      Elem<T>::unpack(vx[i], x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc[j] = __builtin_fmaf(p, x[j], acc[j]);
+    }
+    if (st >= 0) load(W.vbase, tn, vx);
+  }
+#pragma unroll
+  for (int off = LPR; off < 64; off <<= 1) {
+    const float mo = __shfl_xor(m, off), no = __shfl_xor(n, off);
+    float x[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) x[j] = __shfl_xor(acc[j], off);
+    fold<E>(m, n, acc, mo, no, x);
+  }
+  if (lane < LPR) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) out[E * li + j] = acc[j];
+  }
+  if (lane == 0) {
+    *om = m;
+    *on = n;
+  }
+}
+
+// 2 to 16 rows that share the item's chunks: S^T = K Q^T and O^T += V^T P^T,
+// tokens, then channels, as rows and query rows as columns, so P stays in the
+// registers S^T came out in: tokens 4g .. 4g + 3 of each 16.
+template <int S, int D>
+__device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, int nr, const typename Traits<S>::T* qrow,
+                                            int wv, int lane, char* vlds, float* out, float* om, float* on) {
+  using T = typename Traits<S>::T;
+  constexpr bool kF16 = S == kStoreF16, kF32 = S == kStoreF32, kQ4 = S == kStoreKv4;
+  constexpr int TP = kF32 ? 1 : 2;  // tiles of a step
+  constexpr int KS = D / 32, DT = D / 16;
+  constexpr int VS = D + 16, OS = D + 4;
+  constexpr int ES = static_cast<int>(sizeof(T));
+  const int n16 = lane & 15, g = lane >> 4;
+  // 4-bit, up to 8 rows: columns 8 .. 15 repeat them and take the part of P
+  // that fp16 rounds off; with more rows it takes matrix ops of its own
+  const bool half = kQ4 && nr <= 8;
+  const bool low_part = half && n16 >= 8;
+
+  half8 qf[kF32 ? 1 : KS];
+  floatx4 qx[kF32 ? D / 16 : 1];
+  float qk = A.qscale, ql = 0.f;
+  if constexpr (kF32) {
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) qx[u] = *reinterpret_cast<const floatx4*>(qrow + 16 * u + 4 * g);
-  } else if constexpr (S == kStoreF16) {
+  } else if constexpr (kF16) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const half8*>(qrow + 32 * s + 8 * g);
-  } else {
+  } else {  // as for one row
     float amax = 0.f, sum = 0.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -185,130 +482,11 @@ __global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
       for (int i = 0; i < 8; ++i)
         qf[s][i] = static_cast<_Float16>(static_cast<float>(qf[s][i]) * ((i & 2) ? up * 0.0625f : up));
     qk = __builtin_amdgcn_ldexpf(A.qscale, 24 - e);
-    ql = A.qscale * sum;
+    ql = __builtin_amdgcn_ldexpf(sum, e - 24);
   }
 
-  const char* kbase = static_cast<const char*>(A.kpool);
-  const char* vbase = static_cast<const char*>(A.vpool);
-  constexpr int ES = S == kStoreF16 ? 2 : S == kStoreF32 ? 4 : 1;
-  const int64_t ssb = A.ss * ES, hsb = A.hs * ES;
-
-  // tiles per chunk; a step is TP tiles of one chunk, or, over chunks of at
-  // most 16 tokens, one tile each of TP chunks
-  const int tpc = (C + 15) >> 4;
-  const bool small = tpc == 1;
-  const int spc = small ? 1 : (tpc + TP - 1) / TP;  // steps of a chunk (or of TP small ones)
-  const int ngrp = small ? (nch + TP - 1) / TP : nch;
-  const int steps = ngrp * spc;
-  auto place = [&](int st) {
-    Place p;
-    const int c = st / spc, sub = st - c * spc;
-#pragma unroll
-    for (int t = 0; t < TP; ++t) {
-      const int cj = small ? min(c * TP + t, nch - 1) : c;
-      const int tile = small ? 0 : sub * TP + t;
-      p.slot[t] = __builtin_amdgcn_readlane(my.slot, cj);
-      const int start = __builtin_amdgcn_readlane(my.start, cj);
-      const int end = __builtin_amdgcn_readlane(my.end, cj);
-      const bool there = small ? c * TP + t < nch : tile < tpc;
-      p.row[t] = there ? tile * 16 : 0;
-      p.pos[t] = start + p.row[t];
-      p.end[t] = there ? end : 0;
-    }
-    return p;
-  };
-  // nothing of the step is seen, whatever the rows' present lengths
-  auto hidden = [&](const Place& p) {
-    bool hid = true;
-#pragma unroll
-    for (int t = 0; t < TP; ++t) {
-      const int last = min(p.end[t], p.pos[t] + 16) - 1;
-      hid &= last < p.pos[t] || (p.pos[t] >= sinks && last < item.lo);
-    }
-    return hid;
-  };
-  auto next = [&](int st, Place& p) {  // first step at or after st of this wavefront that is seen
-    for (; st < steps; st += 4) {
-      p = place(st);
-      if (!hidden(p)) break;
-    }
-    return st;
-  };
-
-  // Rows past a chunk's last token are loaded all the same (a tile's rows
-  // exist in the pool up to the chunk size; beyond it the last row is read
-  // again) and masked.
-  auto load = [&](Stage<S, D>& x, const Place& p) {
-    if constexpr (S == kStoreF16) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* kt = kbase + p.slot[t] * ssb + h * hsb;
-        const int r = min(p.row[t] + n16, C - 1);
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-          x.k[t][s] = *reinterpret_cast<const half8*>(kt + static_cast<size_t>(r) * (D * 2) + 64 * s + 16 * g);
-      }
-      constexpr int GPR = D / 8, RPL = 64 / GPR;  // granules a row, rows a load
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const int t = i / (D / 32);
-        const int r = min(p.row[t] + (i % (D / 32)) * RPL + lane / GPR, C - 1);
-        x.v[i] = *reinterpret_cast<const u32x4*>(vbase + p.slot[t] * ssb + h * hsb +
-                                                 static_cast<size_t>(r) * (D * 2) + 16 * (lane % GPR));
-      }
-    } else if constexpr (S == kStoreF32) {
-      const char* kt = kbase + p.slot[0] * ssb + h * hsb;
-      const char* vt = vbase + p.slot[0] * ssb + h * hsb;
-      const int r = min(p.row[0] + n16, C - 1);
-#pragma unroll
-      for (int u = 0; u < D / 16; ++u)
-        x.k[u] = *reinterpret_cast<const floatx4*>(kt + static_cast<size_t>(r) * (D * 4) + 64 * u + 16 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int rv = min(p.row[0] + 4 * g + i, C - 1);
-#pragma unroll
-        for (int u = 0; u < D / 64; ++u)
-          x.v[i][u] = *reinterpret_cast<const floatx4*>(vt + static_cast<size_t>(rv) * (D * 4) + 256 * u + 16 * n16);
-      }
-    } else {
-      const int pb = kv4_rows(C) * (D / 2);  // the parameters' place in the tile
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* kt = kbase + p.slot[t] * ssb + h * hsb;
-        const char* vt = vbase + p.slot[t] * ssb + h * hsb;
-        const char* kc = kt + (p.row[t] + n16) * (D / 2) + g * (D / 8);
-        const char* vc = vt + p.row[t] * (D / 2) + lane * (D / 8);
-        if constexpr (D == 128) {
-          const u32x4 a = *reinterpret_cast<const u32x4*>(kc), b = *reinterpret_cast<const u32x4*>(vc);
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            x.k[t][s] = a[s];
-            x.v[t][s] = b[s];
-          }
-        } else {
-          const u32x2 a = *reinterpret_cast<const u32x2*>(kc), b = *reinterpret_cast<const u32x2*>(vc);
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            x.k[t][s] = a[s];
-            x.v[t][s] = b[s];
-          }
-        }
-        x.kp[t] = *reinterpret_cast<const u32x4*>(kt + pb + (p.row[t] + 4 * g) * 4);
-        x.vp[t] = *reinterpret_cast<const u32x4*>(vt + pb + (p.row[t] + 4 * g) * 4);
-      }
-    }
-  };
-
-  float m_run = kNegBig, n_run = 0.f;
-  float base = 0.f, corr = 0.f;  // 4-bit: sum p (low_v + 8 s_v); sum of rounded weights
-  float s_ref = 0.f;             // 4-bit: scale that stands for kScaleTop (uniform)
-  floatx4 acc[DT];
-#pragma unroll
-  for (int t = 0; t < DT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  _Float16* vl = reinterpret_cast<_Float16*>(lds) + wv * (32 * VS);
-
   // bounds over the item's rows: a tile inside them needs no mask
-  int lo_max = lo, lo_min = lo, len_min = len, len_max = len;
+  int lo_max = W.lo, lo_min = W.lo, len_min = W.len, len_max = W.len;
 #pragma unroll
   for (int x = 1; x < 16; x <<= 1) {
     lo_max = max(lo_max, __shfl_xor(lo_max, x));
@@ -321,111 +499,237 @@ __global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
   len_min = __builtin_amdgcn_readfirstlane(len_min);
   len_max = __builtin_amdgcn_readfirstlane(len_max);
 
-  auto compute = [&](Stage<S, D>& x, const Place& p) {
-    bool whole[TP], all = true;
+  half8 kh[kF16 ? 2 : 1][kF16 ? KS : 1];
+  u32x4 vh[kF16 ? D / 16 : 1];
+  floatx4 kf[kF32 ? D / 16 : 1], vf[kF32 ? 4 : 1][kF32 ? D / 64 : 1];
+  uint32_t kc[kQ4 ? 2 : 1][kQ4 ? KS : 1], vc[kQ4 ? 2 : 1][kQ4 ? KS : 1];
+  u32x4 kp[kQ4 ? 2 : 1], vp[kQ4 ? 2 : 1];
+  Tile tn[TP], tc[TP];
+  const int pb = kv4_rows(W.C) * (D / 2);
+  auto words = [&](const char* at, uint32_t* x) {
+    if constexpr (D == 128) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[s] = a[s];
+    } else {
+      const u32x2 a = *reinterpret_cast<const u32x2*>(at);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[s] = a[s];
+    }
+  };
+  auto load_k = [&]() {
 #pragma unroll
     for (int t = 0; t < TP; ++t) {
-      const int last = p.pos[t] + 16;
-      whole[t] = last <= p.end[t] && last <= len_min && (p.pos[t] >= lo_max || last <= sinks);
-      all &= whole[t];
+      const char* kt = W.kbase + tn[t].slot * W.ssb;
+      if constexpr (kQ4) {
+        words(kt + (tn[t].row + n16) * (D / 2) + g * (D / 8), kc[t]);
+        kp[t] = *reinterpret_cast<const u32x4*>(kt + pb + (tn[t].row + 4 * g) * 4);
+      } else {
+        const char* at = kt + static_cast<size_t>(min(tn[t].row + n16, W.C - 1)) * (D * ES) + 16 * g;
+        if constexpr (kF16) {
+#pragma unroll
+          for (int s = 0; s < KS; ++s) kh[t][s] = *reinterpret_cast<const half8*>(at + 64 * s);
+        } else {
+#pragma unroll
+          for (int u = 0; u < D / 16; ++u) kf[u] = *reinterpret_cast<const floatx4*>(at + 64 * u);
+        }
+      }
     }
-    // token i of this lane's four in tile t, seen by row (l, b): by any row
-    // with the extreme bounds
-    auto seen = [&](int t, int i, int l, int b) {
-      const int j = p.pos[t] + i;
-      return j < p.end[t] && j < l && (j >= b || j < sinks);
-    };
+  };
+  auto load_v = [&]() {
+    if constexpr (kQ4) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const char* vt = W.vbase + tn[t].slot * W.ssb;
+        words(vt + tn[t].row * (D / 2) + lane * (D / 8), vc[t]);
+        vp[t] = *reinterpret_cast<const u32x4*>(vt + pb + (tn[t].row + 4 * g) * 4);
+      }
+    } else if constexpr (kF16) {
+      constexpr int GPR = D / 8, RPL = 64 / GPR;  // granules a row, rows a load
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const Tile& t = tn[i / (D / 32)];
+        const int r = min(t.row + (i % (D / 32)) * RPL + lane / GPR, W.C - 1);
+        vh[i] = *reinterpret_cast<const u32x4*>(W.vbase + t.slot * W.ssb + static_cast<size_t>(r) * (D * 2) +
+                                                16 * (lane % GPR));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = min(tn[0].row + 4 * g + i, W.C - 1);
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u)
+          vf[i][u] = *reinterpret_cast<const floatx4*>(W.vbase + tn[0].slot * W.ssb +
+                                                       static_cast<size_t>(r) * (D * 4) + 256 * u + 16 * n16);
+      }
+    }
+  };
+  auto next = [&](int st) {
+    const int steps = (W.n_tiles + TP - 1) / TP;
+    for (; st < steps; st += 4) {
+      bool hid = true;
+#pragma unroll
+      for (int t = 0; t < TP; ++t) {
+        tn[t] = tile_at(W, TP * st + t);
+        hid &= tile_hidden(W, tn[t]);
+      }
+      if (!hid) break;
+    }
+    return st < steps ? st : -1;
+  };
+  // token k of tile t, seen by a row of length l whose window starts at b
+  auto seen = [&](int t, int k, int l, int b) {
+    const int j = tc[t].pos + k;
+    return j < tc[t].end && j < l && (j >= b || j < W.sinks);
+  };
+
+  float m_run = kNegBig, n_run = 0.f;
+  float m_sc = kNegBig, base = 0.f, s_ref = 0.f;  // 4-bit: as for one row
+  floatx4 acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  _Float16* vl = reinterpret_cast<_Float16*>(vlds);
+
+  int st = next(wv);
+  if (st >= 0) {
+    load_k();
+    load_v();
+  }
+  while (st >= 0) {
+#pragma unroll
+    for (int t = 0; t < TP; ++t) tc[t] = tn[t];
+    bool all = true;
+#pragma unroll
+    for (int t = 0; t < TP; ++t) {
+      const int last = tc[t].pos + 16;
+      all &= last <= tc[t].end && last <= len_min && (tc[t].pos >= lo_max || last <= W.sinks);
+    }
     float sc[TP][4];
 #pragma unroll
     for (int t = 0; t < TP; ++t) {
       floatx4 a = {0.f, 0.f, 0.f, 0.f};
-      if constexpr (S == kStoreF32) {
+      if constexpr (kF32) {
 #pragma unroll
         for (int u = 0; u < D / 16; ++u)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            a = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[u][j], qx[u][j], a, 0, 0, 0);
+          for (int j = 0; j < 4; ++j) a = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[u][j], qx[u][j], a, 0, 0, 0);
       } else {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          half8 kk;
-          if constexpr (S == kStoreF16) kk = x.k[t][s];
-          else kk = unpack8(x.k[t][s]);
-          a = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk, qf[s], a, 0, 0, 0);
+          half8 x;
+          if constexpr (kF16) x = kh[t][s];
+          else x = unpack8(kc[t][s]);
+          a = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qf[s], a, 0, 0, 0);
         }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (S == kStoreKv4) {
-          const half2v kp = param(x.kp[t], i);
-          sc[t][i] = __builtin_fmaf(a[i], static_cast<float>(kp[0]) * qk, static_cast<float>(kp[1]) * ql);
+        if constexpr (kQ4) {
+          const half2v y = param(kp[t], i);
+          sc[t][i] = qk * __builtin_fmaf(a[i], static_cast<float>(y[0]), static_cast<float>(y[1]) * ql);
         } else {
-          sc[t][i] = a[i] * A.qscale;
+          sc[t][i] = a[i] * qk;
         }
       }
-      if (!whole[t]) {
+    }
+    const int st_next = next(st + 4);
+    if (st_next >= 0) load_k();
+    float sv[kQ4 ? 2 : 1][4], lv[kQ4 ? 2 : 1][4];
+    float smax = 0.f;
+    if constexpr (kQ4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!seen(t, 4 * g + i, len, lo)) sc[t][i] = -INFINITY;
-      }
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const half2v y = param(vp[t], i);
+          sv[t][i] = static_cast<float>(y[0]);
+          lv[t][i] = static_cast<float>(y[1]);
+        }
+    }
+    if (!all) {
+      rare();
+#pragma unroll
+      for (int t = 0; t < TP; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool vis = seen(t, 4 * g + i, W.len, W.lo);
+          sc[t][i] = vis ? sc[t][i] : -INFINITY;
+          if constexpr (kQ4) {  // whatever is stored where nothing is seen
+            sv[t][i] = vis ? sv[t][i] : 0.f;
+            lv[t][i] = vis ? lv[t][i] : 0.f;
+          }
+        }
     }
     float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < TP; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[t][i]);
-    mx = rows4_max(mx);
-    const float mn = mx > m_run + kLazy ? mx : m_run;
-    if (__any(mn != m_run)) {
-      const float al = fast_exp2(m_run - mn);
+      for (int i = 0; i < 4; ++i) {
+        mx = fmaxf(mx, sc[t][i]);
+        if constexpr (kQ4) smax = fmaxf(smax, sv[t][i]);
+      }
+    const float ref = kQ4 ? m_sc : m_run;
+    if (__any(mx > ref + kLazy || (kQ4 && smax > s_ref))) {
+      rare();
+      mx = rows4_max(mx);
+      float m_new = mx > ref + kLazy ? mx : ref;
+      if constexpr (kQ4) {
+        m_sc = m_new;
+        const float sx = wave_max(smax);
+        if (sx > s_ref) s_ref = 2.f * sx;
+        if (s_ref > 0.f) m_new += __builtin_amdgcn_logf(s_ref) - kScaleTop;
+      }
+      const float al = fast_exp2(m_run - m_new);
       n_run *= al;
       base *= al;
-      corr *= al;
 #pragma unroll
       for (int t = 0; t < DT; ++t) acc[t] *= al;
-      m_run = mn;
+      m_run = m_new;
     }
     float pr[TP][4];
 #pragma unroll
     for (int t = 0; t < TP; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pr[t][i] = fast_exp2(sc[t][i] - m_run);
+      for (int i = 0; i < 4; ++i) {
+        pr[t][i] = fast_exp2(sc[t][i] - m_run);
+        if constexpr (!kF16) n_run += pr[t][i];
+      }
 
-    if constexpr (S == kStoreF32) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) n_run += pr[0][i];
+    // A token that some rows see and others do not: where its V is not finite
+    // (never in ordinary data), 0 * V would reach the others. It counts as 0
+    // then, and o is NaN for the rows that see it: where the product of "not
+    // finite" and "seen" is not zero.
+    if constexpr (kF32) {
       if (!all) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!seen(0, 4 * g + i, len_max, lo_min))
-#pragma unroll
-            for (int u = 0; u < D / 64; ++u) x.v[i][u] = floatx4{0.f, 0.f, 0.f, 0.f};
-        // a token that some rows see and others do not: where its V is not
-        // finite, 0 * V would reach the others, so each column gets its own
-        // operand (never in ordinary data)
+        rare();
         bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          const bool any_row = seen(0, 4 * g + i, len_max, lo_min);
 #pragma unroll
           for (int u = 0; u < D / 64; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) bad |= !(fabsf(x.v[i][u][j]) < INFINITY);
-        if (nr > 1 && __any(bad)) {
-          for (int c = 0; c < nr; ++c) {
-            const int lc = __builtin_amdgcn_readlane(len, c), bc = __builtin_amdgcn_readlane(lo, c);
+            for (int j = 0; j < 4; ++j) {
+              vf[i][u][j] = any_row ? vf[i][u][j] : 0.f;
+              bad |= !(fabsf(vf[i][u][j]) < INFINITY);
+            }
+        }
+        if (__any(bad)) {
 #pragma unroll
-            for (int u = 0; u < D / 64; ++u)
+          for (int u = 0; u < D / 64; ++u)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                floatx4 tmp = {0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 4; ++j) {
+              floatx4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  tmp = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                      seen(0, 4 * g + i, lc, bc) ? x.v[i][u][j] : 0.f, pr[0][i], tmp, 0, 0, 0);
-                if (n16 == c) acc[4 * u + j] += tmp;
+              for (int i = 0; i < 4; ++i) {
+                const bool x = !(fabsf(vf[i][u][j]) < INFINITY);
+                z = __builtin_amdgcn_mfma_f32_16x16x4f32(x ? 1.f : 0.f, seen(0, 4 * g + i, W.len, W.lo) ? 1.f : 0.f,
+                                                         z, 0, 0, 0);
+                vf[i][u][j] = x ? 0.f : vf[i][u][j];
               }
-          }
-          return;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[4 * u + j][i] = z[i] > 0.f ? __builtin_nanf("") : acc[4 * u + j][i];
+            }
         }
       }
 #pragma unroll
@@ -434,23 +738,27 @@ __global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
         for (int u = 0; u < D / 64; ++u)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            acc[4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[i][u][j], pr[0][i], acc[4 * u + j], 0, 0, 0);
-    } else if constexpr (S == kStoreF16) {
-      half8 pb;
+            acc[4 * u + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][u][j], pr[0][i], acc[4 * u + j], 0, 0, 0);
+    } else if constexpr (kF16) {
+      half8 pf;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          pb[4 * t + i] = static_cast<_Float16>(pr[t][i]);
-          n_run += static_cast<float>(pb[4 * t + i]);
+          pf[4 * t + i] = static_cast<_Float16>(pr[t][i]);
+          n_run += static_cast<float>(pf[4 * t + i]);
         }
       constexpr int GPR = D / 8, RPL = 64 / GPR;
+      if (!all) {
+        rare();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          if (!seen(i / (D / 32), (i % (D / 32)) * RPL + lane / GPR, len_max, lo_min)) vh[i] = u32x4{0, 0, 0, 0};
+      }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
-        const int t = i / (D / 32), r = (i % (D / 32)) * RPL + lane / GPR;
-        u32x4 y = x.v[i];
-        if (!all && !seen(t, r, len_max, lo_min)) y = u32x4{0, 0, 0, 0};
-        *reinterpret_cast<u32x4*>(vl + (16 * t + r) * VS + 8 * (lane % GPR)) = y;
+        const int r = 16 * (i / (D / 32)) + (i % (D / 32)) * RPL + lane / GPR;
+        *reinterpret_cast<u32x4*>(vl + r * VS + 8 * (lane % GPR)) = vh[i];
       }
       // the wavefront's own tile: its LDS ops complete in order
       compiler_fence();
@@ -462,123 +770,81 @@ __global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
         va[d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       }
       compiler_fence();
-      if (!all && nr > 1) {
+      if (!all) {
+        rare();
         bool bad = false;
 #pragma unroll
         for (int d = 0; d < DT; ++d) bad |= any_nonfinite(va[d]);
-        if (__any(bad)) {  // as for fp32 above
-          for (int c = 0; c < nr; ++c) {
-            const int lc = __builtin_amdgcn_readlane(len, c), bc = __builtin_amdgcn_readlane(lo, c);
+        if (__any(bad)) {
+          half8 vis;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              half8 vc = va[d];
+          for (int k = 0; k < 8; ++k)
+            vis[k] = static_cast<_Float16>(seen(k / 4, 4 * g + k % 4, W.len, W.lo) ? 1.f : 0.f);
 #pragma unroll
-              for (int k = 0; k < 8; ++k)
-                if (!seen(k / 4, 4 * g + k % 4, lc, bc)) vc[k] = static_cast<_Float16>(0.f);
-              const floatx4 tmp =
-                  __builtin_amdgcn_mfma_f32_16x16x32_f16(vc, pb, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-              if (n16 == c) acc[d] += tmp;
+          for (int d = 0; d < DT; ++d) {
+            half8 x;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const bool b = !(fabsf(static_cast<float>(va[d][k])) < INFINITY);
+              x[k] = static_cast<_Float16>(b ? 1.f : 0.f);
+              va[d][k] = b ? static_cast<_Float16>(0.f) : va[d][k];
             }
+            const floatx4 z = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, vis, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[d][i] = z[i] > 0.f ? __builtin_nanf("") : acc[d][i];
           }
-          return;
         }
       }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pb, acc[d], 0, 0, 0);
+      for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pf, acc[d], 0, 0, 0);
     } else {
-      float sv[2][4], lv[2][4];
-      float smax = 0.f;
+      half8 pf, pl;  // P s_v: rounded; what is left, where it has ops of its own
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const half2v vp = param(x.vp[t], i);
-          sv[t][i] = static_cast<float>(vp[0]);
-          lv[t][i] = static_cast<float>(vp[1]);
-          if (!whole[t]) {
-            // a place without a token, or one this row does not see: whatever
-            // is stored there adds nothing
-            const bool on = seen(t, 4 * g + i, len, lo);
-            sv[t][i] = on ? sv[t][i] : 0.f;
-            lv[t][i] = on ? lv[t][i] : 0.f;
-          }
-          smax = fmaxf(smax, sv[t][i]);
-        }
-      if (__any(smax > s_ref)) {
-        const float s_new = wave_max(smax) * 2.f;
-        const float al = s_ref / s_new;  // s_new > s_ref >= 0
-        corr *= al;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] *= al;
-        s_ref = s_new;
-      }
-      const float f = s_ref > 0.f ? kScaleTop / s_ref : 0.f;
-      half8 pb;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          n_run += pr[t][i] + pr[t][i + 1];
-          base = __builtin_fmaf(pr[t][i], __builtin_fmaf(8.f, sv[t][i], lv[t][i]), base);
-          base = __builtin_fmaf(pr[t][i + 1], __builtin_fmaf(8.f, sv[t][i + 1], lv[t][i + 1]), base);
-          const float u = i ? f * 0.0625f : f;  // the second pair's codes stand 2^4 higher
-          const half2v w = {static_cast<_Float16>(pr[t][i] * sv[t][i] * u),
-                            static_cast<_Float16>(pr[t][i + 1] * sv[t][i + 1] * u)};
-          const _Float16 one = static_cast<_Float16>(i ? 16.f : 1.f);
-          corr = __builtin_amdgcn_fdot2(w, half2v{one, one}, corr, false);
-          pb[4 * t + i] = w[0];
-          pb[4 * t + i + 1] = w[1];
+          base = __builtin_fmaf(pr[t][i], lv[t][i], base);
+          const float w = pr[t][i] * sv[t][i] * (i & 2 ? 0.0625f : 1.f);  // these codes stand 2^4 higher
+          const float hi = top11(w);
+          pf[4 * t + i] = static_cast<_Float16>(low_part ? w - hi : hi);
+          pl[4 * t + i] = static_cast<_Float16>(w - hi);
         }
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const half8 a = unpack8(x.v[0][s]), b = unpack8(x.v[1][s]);
-        const half8 even = __builtin_shufflevector(a, b, 0, 1, 2, 3, 8, 9, 10, 11);
-        const half8 odd = __builtin_shufflevector(a, b, 4, 5, 6, 7, 12, 13, 14, 15);
-        acc[2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pb, acc[2 * s], 0, 0, 0);
-        acc[2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pb, acc[2 * s + 1], 0, 0, 0);
+        const half8 x = unpack8(vc[0][s]), y = unpack8(vc[1][s]);
+        const half8 even = __builtin_shufflevector(x, y, 0, 1, 2, 3, 8, 9, 10, 11);
+        const half8 odd = __builtin_shufflevector(x, y, 4, 5, 6, 7, 12, 13, 14, 15);
+        acc[2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pf, acc[2 * s], 0, 0, 0);
+        acc[2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pf, acc[2 * s + 1], 0, 0, 0);
+        if (!half) {
+          acc[2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pl, acc[2 * s], 0, 0, 0);
+          acc[2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pl, acc[2 * s + 1], 0, 0, 0);
+        }
       }
     }
-  };
-
-  {
-    Stage<S, D> xa, xb;
-    Place pa, pb;
-    int sa = next(wv, pa);
-    if (sa < steps) load(xa, pa);
-    while (sa < steps) {
-      const int sb = next(sa + 4, pb);
-      if (sb < steps) load(xb, pb);
-      compute(xa, pa);
-      if (sb >= steps) break;
-      sa = next(sb + 4, pa);
-      if (sa < steps) load(xa, pa);
-      compute(xb, pb);
-    }
+    st = st_next;
+    if (st >= 0) load_v();
   }
 
-  // Fold the four wavefronts (Eqn 2) through LDS: [wave][row][channel].
-  float n_col = n_run;
-  n_col += __shfl_xor(n_col, 16);
-  n_col += __shfl_xor(n_col, 32);
-  if constexpr (S == kStoreKv4) {
+  n_run += __shfl_xor(n_run, 16);
+  n_run += __shfl_xor(n_run, 32);
+  if constexpr (kQ4) {
     base += __shfl_xor(base, 16);
     base += __shfl_xor(base, 32);
-    corr += __shfl_xor(corr, 16);
-    corr += __shfl_xor(corr, 32);
-    const float back = s_ref * (1.f / kScaleTop);
-    const float off = base - 8.f * corr * back;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[d][i] = __builtin_fmaf(acc[d][i], 16777216.f * back, off);
+      for (int i = 0; i < 4; ++i) {
+        const float o = half ? acc[d][i] + __shfl_xor(acc[d][i], 8) : acc[d][i];
+        acc[d][i] = __builtin_fmaf(o, 16777216.f, base);
+      }
   }
-  if constexpr (S == kStoreF16) __syncthreads();  // the V tiles' place is used again
-  float* mb = reinterpret_cast<float*>(lds);
+  if (kF16) __syncthreads();  // the V tiles' place is used again
   if (n16 < nr) {
-    float* at = mb + (wv * kPlanRows + n16) * OS;
+    float* at = out + n16 * OS;
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      if constexpr (S == kStoreF32) {
+      if constexpr (kF32) {
         // op tile 4u + j, element i: channel 64u + 16g + 4i + j
 #pragma unroll
         for (int i = 0; i < 4; ++i) at[64 * (d / 4) + 16 * g + 4 * i + d % 4] = acc[d][i];
@@ -587,10 +853,63 @@ __global__ __launch_bounds__(256) void kwd_kernel(PlanArgs A) {
       }
     }
     if (g == 0) {
-      s_m[wv][n16] = m_run;
-      s_n[wv][n16] = n_col;
+      om[n16] = m_run;
+      on[n16] = n_run;
     }
   }
+}
+
+template <int S, int D>
+__global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) void kwd_kernel(PlanArgs A) {
+  using T = typename Traits<S>::T;
+  constexpr int OS = D + 4;                    // merge buffer row stride (floats)
+  constexpr int VB = S == kStoreF16 ? 4 * 32 * (D + 16) * 2 : S == kStoreKv4 ? 4 * 256 : 0;
+  constexpr int MB = 4 * kPlanRows * OS * 4;
+  constexpr int LDS = S == kStoreKv4 ? VB + MB : VB > MB ? VB : MB;
+  __shared__ __align__(16) char lds[LDS];
+  __shared__ float s_m[4][kPlanRows], s_n[4][kPlanRows];
+  __shared__ int s_last[kPlanRows];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int H = A.H;
+  const int h = static_cast<int>(blockIdx.x % static_cast<unsigned>(H));
+  const int ib = static_cast<int>(blockIdx.x / static_cast<unsigned>(H));
+  const PlanItem item = A.items[ib];
+  const int nr = item.n_rows;
+  constexpr int ES = S == kStoreF16 ? 2 : S == kStoreF32 ? 4 : 1;
+  Work W;
+  // the chunks, one a lane (chunk_stride <= 64)
+  W.my = A.chunks[static_cast<size_t>(ib) * A.chunk_stride + min(lane, A.chunk_stride - 1)];
+  // 4-bit, up to 8 rows: columns 8 .. 15 repeat them
+  const int col = S == kStoreKv4 && nr <= 8 ? lane & 7 : lane & 15;
+  const int row = item.row_begin + min(col, nr - 1);
+  const PlanRow prow = A.rows[row];
+  const int io = A.row_map ? A.row_map[row] : row;
+  W.kbase = static_cast<const char*>(A.kpool) + h * (A.hs * ES);
+  W.vbase = static_cast<const char*>(A.vpool) + h * (A.hs * ES);
+  W.ssb = A.ss * ES;
+  W.nch = item.n_chunks;
+  W.C = A.C;
+  W.tpc = (A.C + 15) >> 4;
+  W.magic = W.tpc > 1 ? 0xffffffffu / static_cast<unsigned>(W.tpc) + 1u : 0u;
+  W.n_tiles = item.n_chunks * W.tpc;
+  W.sinks = A.sinks;
+  W.lo_item = item.lo;
+  W.len = prow.last_start + A.slot_len[prow.last_slot];
+  W.lo = max(0, W.len - A.window);
+  const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
+  float* mb = reinterpret_cast<float*>(lds + (S == kStoreKv4 ? VB : 0));  // [wave][row][OS]
+  if (nr == 1) {
+    float* out = mb + wv * kPlanRows * OS;
+    if constexpr (S == kStoreKv4) row_kv4<D>(A, W, qrow, wv, lane, lds + wv * 256, out, &s_m[wv][0], &s_n[wv][0]);
+    else row_plain<S, D>(A, W, qrow, wv, lane, out, &s_m[wv][0], &s_n[wv][0]);
+  } else {
+    rows_shared<S, D>(A, W, nr, qrow, wv, lane, lds + (S == kStoreF16 ? wv * (32 * (D + 16) * 2) : 0),
+                      mb + wv * kPlanRows * OS, s_m[wv], s_n[wv]);
+  }
+  // Fold the four wavefronts (Eqn 2) through LDS: [wave][row][channel].
+  // Fold the four wavefronts (Eqn 2) through LDS: [wave][row][channel].
   __syncthreads();
   constexpr int TPR = D / 4, NG = 256 / TPR;  // threads a row, rows at once
   const int gi = tid / TPR, ch = 4 * (tid % TPR);
