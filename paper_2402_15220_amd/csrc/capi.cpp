@@ -791,6 +791,7 @@ static ca_status launch_plan_call(ca_cache* cache, const PlanSlot& slot, const v
   a.chunks = reinterpret_cast<const ca::PlanChunk*>(slot.d + slot.o_chunks);
   a.rows = reinterpret_cast<const ca::PlanRow*>(slot.d + slot.o_rows);
   a.n_items = static_cast<int>(slot.plan.items.size());
+  a.n_block_items = slot.plan.n_block_items;
   a.chunk_stride = slot.plan.stride;
   a.window = slot.plan.window;
   a.sinks = slot.plan.sinks;

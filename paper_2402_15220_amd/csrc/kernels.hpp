@@ -167,6 +167,7 @@ struct PlanArgs {
   const PlanChunk* chunks;  // [n_items][chunk_stride]
   const PlanRow* rows;
   int n_items;
+  int n_block_items;  // the first ones: a block a head; the others: a wavefront a head
   int chunk_stride;
   int window;  // positions a query sees besides the sinks (kNoWindow: all)
   int sinks;

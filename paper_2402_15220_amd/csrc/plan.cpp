@@ -5,6 +5,9 @@
 
 namespace ca {
 
+// fewest tokens a wavefront of its own gets
+constexpr int64_t kSoloTokens = 256;
+
 void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t sinks, int32_t heads,
                 int32_t num_cus, Plan* out) {
   Plan& P = *out;
@@ -27,6 +30,7 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
     std::vector<int32_t> seen;  // visible nodes, root -> leaf
     int64_t tokens = 0;
     int32_t pieces = 0;
+    bool solo = false;
   };
   std::vector<Run> runs;
   std::vector<int32_t> run_of(nn);
@@ -53,17 +57,28 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
     }
   }
 
-  // Pieces: about four blocks a compute unit, of at least 128 tokens (one
-  // step of a block's four wavefronts).
-  int64_t load = 0;
-  for (const Run& r : runs)
-    load += (r.row_end - r.row_begin + kPlanRows - 1) / kPlanRows * r.tokens * heads;
-  const int64_t piece_tokens = std::max<int64_t>(128, (load + 4 * num_cus - 1) / (4 * num_cus));
-  P.piece_chunks = static_cast<int32_t>(std::min<int64_t>(kPlanChunks - 2, std::max<int64_t>(1, (piece_tokens + C - 1) / C)));
+  // Pieces: about four blocks a compute unit, of at least 128 tokens. Runs of
+  // one row get a wavefront a head where that leaves a wavefront as many
+  // tokens as it would have with the load spread over all of them, and enough
+  // to pay for its start.
+  int64_t load = 0, own = 0;
+  for (const Run& r : runs) {
+    const int64_t tiles = (r.row_end - r.row_begin + kPlanRows - 1) / kPlanRows;
+    load += tiles * r.tokens * heads;
+    if (r.row_end - r.row_begin == 1) own += r.tokens * heads;
+  }
+  const int64_t waves = 16 * static_cast<int64_t>(num_cus);
+  const int64_t piece_tokens = std::max<int64_t>(128, 4 * load / waves);
+  const int64_t solo_tokens = own / waves >= kSoloTokens ? own / waves * 5 / 2 : 0;
+  auto chunks_of = [&](int64_t tokens) {
+    return static_cast<int32_t>(std::min<int64_t>(kPlanChunks - 2, std::max<int64_t>(1, (tokens + C - 1) / C)));
+  };
   int32_t longest = 0;
   for (Run& r : runs) {
     const int32_t n = static_cast<int32_t>(r.seen.size());
-    r.pieces = (n + P.piece_chunks - 1) / P.piece_chunks;
+    r.solo = r.row_end - r.row_begin == 1 && r.tokens <= solo_tokens;
+    const int32_t len = chunks_of(r.solo ? solo_tokens : piece_tokens);
+    r.pieces = (n + len - 1) / len;
     if (r.parent >= 0) r.ord = runs[r.parent].ord + runs[r.parent].pieces;
     if (r.pieces) longest = std::max(longest, (n + r.pieces - 1) / r.pieces);
   }
@@ -79,11 +94,13 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
     if (np > 1) P.n_parts += np;
   }
 
-  // Shared runs first: their blocks work on up to 16 rows each.
-  for (int pass = 0; pass < 2; ++pass) {
+  // Shared runs first: their blocks work on up to 16 rows each; then single
+  // rows, those of a wavefront a head last.
+  for (int pass = 0; pass < 3; ++pass) {
+    if (pass == 2) P.n_block_items = static_cast<int32_t>(P.items.size());
     for (const Run& r : runs) {
       const bool shared = r.row_end - r.row_begin > 1;
-      if (shared != (pass == 0)) continue;
+      if (pass != (shared ? 0 : r.solo ? 2 : 1)) continue;
       const int32_t n = static_cast<int32_t>(r.seen.size());
       for (int32_t k = 0; k < r.pieces; ++k) {
         const int32_t c0 = static_cast<int32_t>(static_cast<int64_t>(n) * k / r.pieces);

@@ -5,8 +5,11 @@
 // The tree is cut into runs (maximal chains of chunks that the same rows
 // cover). Of each run the chunks that some row sees, at the time the plan is
 // made, are cut into pieces of about the same number of tokens, and the run's
-// rows into tiles of up to 16; an item is one piece and one tile, and one
-// block of the launch is an item of one head. Sequences only grow while the
+// rows into tiles of up to 16; an item is one piece and one tile. Of most
+// items a block of the launch works on one head, its four wavefronts on the
+// tokens in turn; where single rows are long and many enough, a wavefront
+// takes a head of an item to itself and a block four heads (no fold, and what
+// a wavefront does once is spread over four times the tokens). Sequences only grow while the
 // plan stands, so their windows only move forward and what it lists stays a
 // superset of what they see; the kernel masks by the lengths on the device.
 //
@@ -59,7 +62,7 @@ struct Plan {
   int32_t stride = 0;
   int32_t n_parts = 0;
   int32_t window = 0, sinks = 0;
-  int32_t piece_chunks = 0;
+  int32_t n_block_items = 0;  // items whose tokens a block's four wavefronts share
 };
 
 // heads x items is the launch; num_cus sizes the pieces.

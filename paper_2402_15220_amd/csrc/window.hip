@@ -139,7 +139,7 @@ __device__ __forceinline__ bool tile_hidden(const Work& W, const Tile& t) {
 // the lanes that need it as B operand, its rounded part in even columns, the
 // rest in odd ones, so P loses nothing to fp16.
 template <int D>
-__device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const _Float16* qrow, int wv, int lane,
+__device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const _Float16* qrow, int wv, int nw, int lane,
                                         char* plds, float* out, float* om, float* on) {
   constexpr int KS = D / 32, DT = D / 16;
   const int n16 = lane & 15, g = lane >> 4;
@@ -213,7 +213,7 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
   };
   auto next = [&](int st) {
     const int steps = (W.n_tiles + 3) / 4;
-    for (; st < steps; st += 4) {
+    for (; st < steps; st += nw) {
       fetch(st);
       if (!(tile_hidden(W, tn[0]) && tile_hidden(W, tn[1]) && tile_hidden(W, tn[2]) && tile_hidden(W, tn[3]))) break;
     }
@@ -245,7 +245,7 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
     const float raw = g & 2 ? (g & 1 ? a[3][0] : a[2][0]) : (g & 1 ? a[1][0] : a[0][0]);
     const half2v kq = __builtin_bit_cast(half2v, kp);
     const int pos = pos_n, end = end_n;
-    st = next(st + 4);
+    st = next(st + nw);
     if (st >= 0) load_k();
     const bool on = pos < end && pos < W.len && (pos >= W.lo || pos < W.sinks);
     float sc = qk * __builtin_fmaf(raw, static_cast<float>(kq[0]), static_cast<float>(kq[1]) * ql);
@@ -315,7 +315,7 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
 // rows it saw, with P in 32 bits; the groups are folded at the end.
 template <int S, int D>
 __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, const typename Traits<S>::T* qrow, int wv,
-                                          int lane, float* out, float* om, float* on) {
+                                          int nw, int lane, float* out, float* om, float* on) {
   using T = typename Traits<S>::T;
   constexpr int E = 16 / sizeof(T);                 // elements of a lane
   constexpr int LPR = D / E, RPL = 64 / LPR;
@@ -343,7 +343,7 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
   };
   auto next = [&](int st) {
     const int steps = (W.n_tiles + TP - 1) / TP;
-    for (; st < steps; st += 4) {
+    for (; st < steps; st += nw) {
       fetch(st);
       bool hid = true;
 #pragma unroll
@@ -373,7 +373,7 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
       for (int j = 0; j < E; ++j) d = __builtin_fmaf(x[j], qv[j], d);
       sc[i] = group_sum<LPR>(d) * A.qscale;
     }
-    st = next(st + 4);
+    st = next(st + nw);
     if (st >= 0) load(W.kbase, tn, kx);
     bool all = true;
 #pragma unroll
@@ -868,13 +868,26 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
   constexpr int LDS = S == kStoreKv4 ? VB + MB : VB > MB ? VB : MB;
   __shared__ __align__(16) char lds[LDS];
   __shared__ float s_m[4][kPlanRows], s_n[4][kPlanRows];
-  __shared__ int s_last[kPlanRows];
+  __shared__ int s_last[kPlanRows], s_pbase[kPlanRows], s_np[kPlanRows], s_io[kPlanRows];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int H = A.H;
-  const int h = static_cast<int>(blockIdx.x % static_cast<unsigned>(H));
-  const int ib = static_cast<int>(blockIdx.x / static_cast<unsigned>(H));
+  // An item of a block: one head of it, the wavefronts share its tokens. An
+  // item of wavefronts: four heads of it, one a wavefront.
+  const int b = static_cast<int>(blockIdx.x), n_blk = A.n_block_items * H;
+  const bool solo = b >= n_blk;
+  int ib, h0;
+  if (solo) {
+    const int hb = (H + 3) >> 2;
+    ib = (b - n_blk) / hb;
+    h0 = 4 * (b - n_blk - ib * hb);
+    ib += A.n_block_items;
+  } else {
+    ib = b / H;
+    h0 = b - ib * H;
+  }
+  const int h = solo ? min(h0 + wv, H - 1) : h0;  // a wavefront past the heads repeats the last one
   const PlanItem item = A.items[ib];
   const int nr = item.n_rows;
   constexpr int ES = S == kStoreF16 ? 2 : S == kStoreF32 ? 4 : 1;
@@ -898,26 +911,35 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
   W.lo_item = item.lo;
   W.len = prow.last_start + A.slot_len[prow.last_slot];
   W.lo = max(0, W.len - A.window);
+  if (tid < kPlanRows) {
+    s_pbase[tid] = prow.pbase;
+    s_np[tid] = prow.np;
+    s_io[tid] = io;
+  }
   const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
   float* mb = reinterpret_cast<float*>(lds + (S == kStoreKv4 ? VB : 0));  // [wave][row][OS]
   if (nr == 1) {
     float* out = mb + wv * kPlanRows * OS;
-    if constexpr (S == kStoreKv4) row_kv4<D>(A, W, qrow, wv, lane, lds + wv * 256, out, &s_m[wv][0], &s_n[wv][0]);
-    else row_plain<S, D>(A, W, qrow, wv, lane, out, &s_m[wv][0], &s_n[wv][0]);
+    const int w0 = solo ? 0 : wv, nw = solo ? 1 : 4;
+    if constexpr (S == kStoreKv4) row_kv4<D>(A, W, qrow, w0, nw, lane, lds + wv * 256, out, &s_m[wv][0], &s_n[wv][0]);
+    else row_plain<S, D>(A, W, qrow, w0, nw, lane, out, &s_m[wv][0], &s_n[wv][0]);
   } else {
     rows_shared<S, D>(A, W, nr, qrow, wv, lane, lds + (S == kStoreF16 ? wv * (32 * (D + 16) * 2) : 0),
                       mb + wv * kPlanRows * OS, s_m[wv], s_n[wv]);
   }
-  // Fold the four wavefronts (Eqn 2) through LDS: [wave][row][channel].
-  // Fold the four wavefronts (Eqn 2) through LDS: [wave][row][channel].
+  // Result r of the block: row r of the item, folded from the four wavefronts
+  // (Eqn 2) through LDS, [wave][row][channel]; or, of an item of wavefronts,
+  // head h0 + r as wavefront r left it.
   __syncthreads();
-  constexpr int TPR = D / 4, NG = 256 / TPR;  // threads a row, rows at once
+  constexpr int TPR = D / 4, NG = 256 / TPR;  // threads a result, results at once
   const int gi = tid / TPR, ch = 4 * (tid % TPR);
+  const int n_res = solo ? min(4, H - h0) : nr;
   const __amdgpu_buffer_rsrc_t rs = part_rsrc(A.ws_o, A.ws_o_bytes);
   T* out = static_cast<T*>(A.o);
-  auto write_row = [&](int row, const floatx4& v, float n) {
-    const int r = A.row_map ? A.row_map[row] : row;
-    T* at = out + (static_cast<size_t>(r) * H + h) * D + ch;
+  auto row_of = [&](int r) { return solo ? 0 : r; };
+  auto head_of = [&](int r) { return solo ? h0 + r : h0; };
+  auto write_row = [&](int r, const floatx4& v, float n) {
+    T* at = out + (static_cast<size_t>(s_io[row_of(r)]) * H + head_of(r)) * D + ch;
     const float inv = 1.f / n;
     if constexpr (S == kStoreF32) {
       *reinterpret_cast<floatx4*>(at) = v * inv;
@@ -928,24 +950,31 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
       *reinterpret_cast<half4*>(at) = y;
     }
   };
-  for (int r = gi; r < nr; r += NG) {
-    float m = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+  bool parts = false;
+  for (int r = gi; r < n_res; r += NG) {
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    float n = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = fast_exp2(s_m[w][r] - m);
-      n += s_n[w][r] * f;
-      v += *reinterpret_cast<const floatx4*>(mb + (w * kPlanRows + r) * OS + ch) * f;
-    }
-    const PlanRow pr = A.rows[item.row_begin + r];
-    if (pr.np == 1) {
-      write_row(item.row_begin + r, v, n);
+    float n = 0.f, m;
+    if (solo) {
+      m = s_m[r][0];
+      n = s_n[r][0];
+      v = *reinterpret_cast<const floatx4*>(mb + r * kPlanRows * OS + ch);
     } else {
-      const int p = pr.pbase + item.ord;
-      st_dev4(rs, ((static_cast<uint32_t>(p) * H + h) * D + ch) * 4u, v[0], v[1], v[2], v[3]);
+      m = fmaxf(fmaxf(s_m[0][r], s_m[1][r]), fmaxf(s_m[2][r], s_m[3][r]));
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = fast_exp2(s_m[w][r] - m);
+        n += s_n[w][r] * f;
+        v += *reinterpret_cast<const floatx4*>(mb + (w * kPlanRows + r) * OS + ch) * f;
+      }
+    }
+    if (s_np[row_of(r)] == 1) {
+      write_row(r, v, n);
+    } else {
+      parts = true;
+      const int p = s_pbase[row_of(r)] + item.ord, hr = head_of(r);
+      st_dev4(rs, ((static_cast<uint32_t>(p) * H + hr) * D + ch) * 4u, v[0], v[1], v[2], v[3]);
       if (ch == 0) {
-        float* ml = A.ws_ml + (static_cast<size_t>(p) * H + h) * 2;
+        float* ml = A.ws_ml + (static_cast<size_t>(p) * H + hr) * 2;
         st_dev(ml, m);
         st_dev(ml + 1, n);
       }
@@ -953,47 +982,60 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
   }
   // Partials: the last block to arrive on a row folds them (the exchange
   // protocol of device_common.hpp).
+  if (!__syncthreads_or(parts)) return;
   wait_stores();
   __syncthreads();
-  if (tid < nr) {
-    const PlanRow pr = A.rows[item.row_begin + tid];
+  if (tid < n_res) {
     bool last = false;
-    if (pr.np > 1) {
-      const int row = item.row_begin + tid;
-      int32_t* c = A.cnt_layout < 0 ? A.cnt + (static_cast<size_t>(row) * H + h)
-                                    : A.cnt + (static_cast<size_t>(row >> A.cnt_layout) * H + h) * 32 +
-                                          (row & ((1 << A.cnt_layout) - 1));
-      last = arrive_last(c, pr.np);
+    if (s_np[row_of(tid)] > 1) {
+      const int r = item.row_begin + row_of(tid), hr = head_of(tid);
+      int32_t* c = A.cnt_layout < 0 ? A.cnt + (static_cast<size_t>(r) * H + hr)
+                                    : A.cnt + (static_cast<size_t>(r >> A.cnt_layout) * H + hr) * 32 +
+                                          (r & ((1 << A.cnt_layout) - 1));
+      last = arrive_last(c, s_np[row_of(tid)]);
     }
     s_last[tid] = last;
   }
   __syncthreads();
-  auto fold_from = [&](int p0, int step, int p1, float& m, float& n, floatx4& v) {
-    for (int p = p0; p < p1; p += step) {
-      const float* ml = A.ws_ml + (static_cast<size_t>(p) * H + h) * 2;
-      const float pm = ld_dev(ml), pn = ld_dev(ml + 1);
-      const float4 x = ld_dev4(rs, ((static_cast<uint32_t>(p) * H + h) * D + ch) * 4u);
-      const float M = fmaxf(m, pm);
-      const float a = fast_exp2(m - M), b = fast_exp2(pm - M);
-      n = n * a + pn * b;
-      v = v * a + floatx4{x.x, x.y, x.z, x.w} * b;
-      m = M;
+  // partials p0, p0 + step, ... below p1 of head hr into (m, n, v), the loads of
+  // four in flight together
+  auto fold_from = [&](int p0, int step, int p1, int hr, float& m, float& n, floatx4& v) {
+    constexpr int NB = 4;
+    for (; p0 < p1; p0 += NB * step) {
+      float pm[NB], pn[NB];
+      float4 x[NB];
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        const int p = min(p0 + k * step, p1 - 1);  // past the end: a valid one, not used
+        const float* ml = A.ws_ml + (static_cast<size_t>(p) * H + hr) * 2;
+        pm[k] = ld_dev(ml);
+        pn[k] = ld_dev(ml + 1);
+        x[k] = ld_dev4(rs, ((static_cast<uint32_t>(p) * H + hr) * D + ch) * 4u);
+      }
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        if (p0 + k * step >= p1) break;
+        const float M = fmaxf(m, pm[k]);
+        const float a = fast_exp2(m - M), c = fast_exp2(pm[k] - M);
+        n = n * a + pn[k] * c;
+        v = v * a + floatx4{x[k].x, x[k].y, x[k].z, x[k].w} * c;
+        m = M;
+      }
     }
   };
-  if (nr > 1) {  // a row to each group of threads
-    for (int r = gi; r < nr; r += NG) {
+  if (nr > 1 || solo) {  // a result to each group of threads
+    for (int r = gi; r < n_res; r += NG) {
       if (!s_last[r]) continue;
-      const PlanRow pr = A.rows[item.row_begin + r];
       float m = kNegBig, n = 0.f;
       floatx4 v = {0.f, 0.f, 0.f, 0.f};
-      fold_from(pr.pbase, 1, pr.pbase + pr.np, m, n, v);
-      write_row(item.row_begin + r, v, n);
+      const int p0 = s_pbase[row_of(r)];
+      fold_from(p0, 1, p0 + s_np[row_of(r)], head_of(r), m, n, v);
+      write_row(r, v, n);
     }
-  } else if (s_last[0]) {  // one row: its partials dealt out to the groups
-    const PlanRow pr = A.rows[item.row_begin];
+  } else if (s_last[0]) {  // one: its partials dealt out to the groups
     float m = kNegBig, n = 0.f;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    fold_from(pr.pbase + gi, NG, pr.pbase + pr.np, m, n, v);
+    fold_from(s_pbase[0] + gi, NG, s_pbase[0] + s_np[0], h0, m, n, v);
     *reinterpret_cast<floatx4*>(mb + gi * OS + ch) = v;
     float* gm = mb + NG * OS;
     if (ch == 0) {
@@ -1011,7 +1053,7 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
         nn += gm[2 * k + 1] * f;
         o += *reinterpret_cast<const floatx4*>(mb + k * OS + ch) * f;
       }
-      write_row(item.row_begin, o, nn);
+      write_row(0, o, nn);
     }
   }
 }
@@ -1021,7 +1063,8 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
 hipError_t launch_plan_attention(const PlanArgs& a, hipStream_t stream) {
   if (a.n_items <= 0) return hipSuccess;
   if (a.chunk_stride < 1 || a.chunk_stride > kPlanChunks) return hipErrorInvalidValue;
-  const unsigned grid = static_cast<unsigned>(a.n_items) * static_cast<unsigned>(a.H);
+  const unsigned grid = static_cast<unsigned>(a.n_block_items) * static_cast<unsigned>(a.H) +
+                        static_cast<unsigned>(a.n_items - a.n_block_items) * static_cast<unsigned>((a.H + 3) / 4);
   auto go = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(a); };
   if (a.D == 128) {
     if (a.store == kStoreF16) go(kwd_kernel<kStoreF16, 128>);
