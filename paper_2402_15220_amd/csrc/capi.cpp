@@ -396,7 +396,7 @@ struct ca_cache {
     if (!at->valid) {
       ca::build_tables(tree, &tables);
       at->uploaded = false;
-      ca::build_plan(tree, tables, window, sinks, cfg.num_heads, num_cus, &at->plan);
+      ca::build_plan(tree, tables, window, sinks, cfg.num_heads, num_cus, kv4() ? 8 : 12, &at->plan);
       at->valid = true;
     }
     return *at;

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
       } else if (mine) {
         const size_t src = static_cast<size_t>(j.src) * ss + static_cast<size_t>(h) * hs;
         const int sr = j.src_pos + row - j.dst_pos;  // source row
-        kw = reinterpret_cast<const uint32_t*>(kpool + src + static_cast<size_t>(sr) * (D / 2))[e];
+        kw = reinterpret_cast<const uint32_t*>(kpool + src)[kv4_k_word(sr, e, D)];
         kp = reinterpret_cast<const uint32_t*>(kpool + src + code_bytes)[sr];
         vp = reinterpret_cast<const uint32_t*>(vpool + src + code_bytes)[sr];
         // elements 8e .. 8e + 7 are channels n0 .. n0 + 7 of tile 2 tp + hb
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
         }
       }
       if (mine) {
-        reinterpret_cast<uint32_t*>(kpool + dst + static_cast<size_t>(row) * (D / 2))[e] = kw;
+        reinterpret_cast<uint32_t*>(kpool + dst)[kv4_k_word(row, e, D)] = kw;
         if (e == 0) {
           reinterpret_cast<uint32_t*>(kpool + dst + code_bytes)[row] = kp;
           reinterpret_cast<uint32_t*>(vpool + dst + code_bytes)[row] = vp;

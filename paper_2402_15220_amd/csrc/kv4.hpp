@@ -6,7 +6,9 @@
 // kv4_rows(C) rows of codes, D/2 bytes each, then one (scale, low) pair of
 // fp16 a row. Codes come in blocks of 16 tokens, laid out as the kernels'
 // matrix operands need them:
-//   K  token-major: the 32-bit word W of a row holds elements 8W .. 8W + 7.
+//   K  word (16 g + n) * D/32 + w holds elements 8W .. 8W + 7 of token n,
+//      W = g * D/32 + w: lane 16 g + n of a wavefront reads its D/32 words at
+//      once, and a wavefront's load is one run of memory.
 //   V  for group g = token % 16 / 4, channel n of each 16 and pair t of
 //      16-channel tiles, word (16 g + n) * D/32 + t holds the codes of the
 //      group's four tokens at channels 32 t + n and 32 t + 16 + n.
@@ -26,5 +28,9 @@ constexpr int64_t kv4_tile_bytes(int C, int D) {
   return static_cast<int64_t>(kv4_rows(C)) * (D / 2 + 4);
 }
 constexpr int kv4_nibble(int k) { return (k >> 1) + 4 * (k & 1); }
+// word of elements 8W .. 8W + 7 of K token t, counted from the tile's start
+constexpr int kv4_k_word(int t, int W, int D) {
+  return (t & ~15) * (D / 8) + (16 * (W / (D / 32)) + (t & 15)) * (D / 32) + W % (D / 32);
+}
 
 }  // namespace ca

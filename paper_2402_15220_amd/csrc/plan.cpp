@@ -5,14 +5,16 @@
 
 namespace ca {
 
-// fewest tokens a wavefront of its own gets
-constexpr int64_t kSoloTokens = 256;
+// Rows of their own go to single wavefronts where those get at least
+// kSoloTokens tokens on average, and where a row has no more than kSoloShort:
+// a block's four wavefronts would mostly wait for each other.
+constexpr int64_t kSoloTokens = 256, kSoloShort = 128;
 
-void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t sinks, int32_t heads,
-                int32_t num_cus, Plan* out) {
+void build_plan(const ChunkTree& tree, const Tables& tab, int32_t window, int32_t sinks, int32_t heads,
+                int32_t num_cus, int32_t waves_per_cu, Plan* out) {
   Plan& P = *out;
-  const int32_t B = static_cast<int32_t>(t.row_seq.size());
-  const int32_t nn = static_cast<int32_t>(t.node_slot.size());
+  const int32_t B = static_cast<int32_t>(tab.row_seq.size());
+  const int32_t nn = static_cast<int32_t>(tab.node_slot.size());
   const int32_t C = tree.chunk_size();
   P = Plan();
   P.window = window;
@@ -20,7 +22,7 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
 
   std::vector<int32_t> lo(B);  // first position of each row's window
   for (int32_t r = 0; r < B; ++r) {
-    const int64_t len = tree.seqs().at(t.row_seq[r]).length;
+    const int64_t len = tree.seqs().at(tab.row_seq[r]).length;
     lo[r] = static_cast<int32_t>(std::max<int64_t>(0, len - window));
   }
 
@@ -35,8 +37,8 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
   std::vector<Run> runs;
   std::vector<int32_t> run_of(nn);
   for (int32_t i = 0; i < nn; ++i) {
-    const int32_t p = t.node_parent[i], rb = t.node_row_begin[i], re = t.node_row_end[i];
-    if (p >= 0 && t.node_row_begin[p] == rb && t.node_row_end[p] == re) {
+    const int32_t p = tab.node_parent[i], rb = tab.node_row_begin[i], re = tab.node_row_end[i];
+    if (p >= 0 && tab.node_row_begin[p] == rb && tab.node_row_end[p] == re) {
       run_of[i] = run_of[p];
     } else {
       run_of[i] = static_cast<int32_t>(runs.size());
@@ -48,7 +50,7 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
       runs.push_back(std::move(r));
     }
     Run& r = runs[run_of[i]];
-    const int32_t start = t.node_start_pos[i], end = start + t.node_len[i];
+    const int32_t start = tab.node_start_pos[i], end = start + tab.node_len[i];
     if (start < sinks || end > r.lo) {
       r.seen.push_back(i);
       // tokens read: the part in the window and the sinks
@@ -57,19 +59,16 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
     }
   }
 
-  // Pieces: about four blocks a compute unit, of at least 128 tokens. Runs of
-  // one row get a wavefront a head where that leaves a wavefront as many
-  // tokens as it would have with the load spread over all of them, and enough
-  // to pay for its start.
+  // Pieces: as many as the chip is to have at once, of at least 128 tokens.
   int64_t load = 0, own = 0;
   for (const Run& r : runs) {
     const int64_t tiles = (r.row_end - r.row_begin + kPlanRows - 1) / kPlanRows;
     load += tiles * r.tokens * heads;
     if (r.row_end - r.row_begin == 1) own += r.tokens * heads;
   }
-  const int64_t waves = 16 * static_cast<int64_t>(num_cus);
+  const int64_t waves = static_cast<int64_t>(waves_per_cu) * num_cus;
   const int64_t piece_tokens = std::max<int64_t>(128, 4 * load / waves);
-  const int64_t solo_tokens = own / waves >= kSoloTokens ? own / waves * 5 / 2 : 0;
+  const int64_t solo_tokens = own / waves >= kSoloTokens ? own / waves * 5 / 2 : kSoloShort;
   auto chunks_of = [&](int64_t tokens) {
     return static_cast<int32_t>(std::min<int64_t>(kPlanChunks - 2, std::max<int64_t>(1, (tokens + C - 1) / C)));
   };
@@ -85,12 +84,13 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
   P.stride = longest + 2;  // room for growth
 
   P.rows.resize(B);
+  P.first_item.assign(B, -1);
   P.last_item.assign(B, -1);
   for (int32_t r = 0; r < B; ++r) {
-    const int32_t leaf = t.path_node[t.path_ptr[r + 1] - 1];
+    const int32_t leaf = tab.path_node[tab.path_ptr[r + 1] - 1];
     const Run& run = runs[run_of[leaf]];
     const int32_t np = run.ord + run.pieces;
-    P.rows[r] = {t.node_slot[leaf], t.node_start_pos[leaf], np > 1 ? P.n_parts : -1, np};
+    P.rows[r] = {tab.node_slot[leaf], tab.node_start_pos[leaf], np > 1 ? P.n_parts : -1, np};
     if (np > 1) P.n_parts += np;
   }
 
@@ -105,18 +105,31 @@ void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t 
       for (int32_t k = 0; k < r.pieces; ++k) {
         const int32_t c0 = static_cast<int32_t>(static_cast<int64_t>(n) * k / r.pieces);
         const int32_t c1 = static_cast<int32_t>(static_cast<int64_t>(n) * (k + 1) / r.pieces);
-        for (int32_t rb = r.row_begin; rb < r.row_end; rb += kPlanRows) {
+        // even tiles: a shared run's never have one row only
+        const int32_t rows = r.row_end - r.row_begin, tiles = (rows + kPlanRows - 1) / kPlanRows;
+        for (int32_t t = 0; t < tiles; ++t) {
+          const int32_t rb = r.row_begin + rows * t / tiles, re = r.row_begin + rows * (t + 1) / tiles;
           const size_t at = P.chunks.size();
           P.chunks.resize(at + P.stride, PlanChunk{0, 0, 0, 0});
           for (int32_t c = c0; c < c1; ++c) {
-            const int32_t i = r.seen[c], start = t.node_start_pos[i];
+            const int32_t i = r.seen[c], start = tab.node_start_pos[i];
             const bool open = !shared && c == n - 1;
-            P.chunks[at + c - c0] = {t.node_slot[i], start, open ? kOpenEnd : start + t.node_len[i], 0};
+            P.chunks[at + c - c0] = {tab.node_slot[i], start, open ? kOpenEnd : start + tab.node_len[i], 0};
           }
-          if (!shared && c1 == n) P.last_item[rb] = static_cast<int32_t>(P.items.size());
-          const int32_t re = std::min(rb + kPlanRows, r.row_end);
+          if (!shared) {
+            P.last_item[rb] = static_cast<int32_t>(P.items.size());
+            if (k == 0) P.first_item[rb] = P.last_item[rb];
+          }
           const int32_t ilo = *std::min_element(lo.begin() + rb, lo.begin() + re);
-          P.items.push_back({rb, re - rb, c1 - c0, r.ord + k, ilo, {0, 0, 0}});
+          PlanItem it{rb, re - rb, c1 - c0, r.ord + k, ilo, 0, 0, -1, 0, {0, 0, 0}};
+          if (!shared) {
+            const PlanRow& pr = P.rows[rb];
+            it.last_slot = pr.last_slot;
+            it.last_start = pr.last_start;
+            it.pbase = pr.pbase;
+            it.np = pr.np;
+          }
+          P.items.push_back(it);
         }
       }
     }
@@ -144,6 +157,10 @@ bool patch_plan(const ChunkTree& tree, const std::unordered_map<int64_t, int32_t
     ++item.n_chunks;
     r.last_slot = nd.slot;
     r.last_start = start;
+    for (int32_t k = p->first_item[row]; k <= i; ++k) {
+      p->items[k].last_slot = nd.slot;
+      p->items[k].last_start = start;
+    }
   }
   return true;
 }

@@ -38,6 +38,8 @@ struct PlanItem {
   int32_t n_chunks;
   int32_t ord;
   int32_t lo;  // no row of the item sees a position below lo that is no sink
+  // of an item of one row, the row's PlanRow (one load less in a row's chain)
+  int32_t last_slot, last_start, pbase, np;
   int32_t pad[3];
 };
 struct PlanChunk {
@@ -52,22 +54,25 @@ struct PlanRow {
   int32_t pbase;       // -1: one piece only
   int32_t np;
 };
-static_assert(sizeof(PlanItem) == 32 && sizeof(PlanChunk) == 16 && sizeof(PlanRow) == 16, "plan layout");
+static_assert(sizeof(PlanItem) == 48 && sizeof(PlanChunk) == 16 && sizeof(PlanRow) == 16, "plan layout");
 
 struct Plan {
   std::vector<PlanItem> items;
   std::vector<PlanChunk> chunks;  // [items][stride]
   std::vector<PlanRow> rows;
-  std::vector<int32_t> last_item;  // per row the item that ends in its last chunk, or -1
+  // per row the items of its own chunks, [first, last], the last one ending in
+  // the row's last chunk; -1: none
+  std::vector<int32_t> first_item, last_item;
   int32_t stride = 0;
   int32_t n_parts = 0;
   int32_t window = 0, sinks = 0;
   int32_t n_block_items = 0;  // items whose tokens a block's four wavefronts share
 };
 
-// heads x items is the launch; num_cus sizes the pieces.
+// heads x items is the launch; the pieces are sized for waves_per_cu wavefronts
+// on each of num_cus compute units.
 void build_plan(const ChunkTree& tree, const Tables& t, int32_t window, int32_t sinks, int32_t heads,
-                int32_t num_cus, Plan* out);
+                int32_t num_cus, int32_t waves_per_cu, Plan* out);
 
 // Append the chunks that decode growth added (tree.grown()) to their rows'
 // last items; false (the plan is then to be rebuilt) where one has no room.

@@ -34,6 +34,7 @@
 
 #include <cfloat>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "kernels.hpp"
@@ -143,32 +144,9 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
                                         char* plds, float* out, float* om, float* on) {
   constexpr int KS = D / 32, DT = D / 16;
   const int n16 = lane & 15, g = lane >> 4;
-  half8 qf[KS];
-  float amax = 0.f, sum = 0.f;
+  half8 qf[KS];  // asked for first, used after the first step's loads are out
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    qf[s] = *reinterpret_cast<const half8*>(qrow + KS * 8 * g + 8 * s);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = static_cast<float>(qf[s][i]);
-      amax = fmaxf(amax, fabsf(x));
-      sum += x;
-    }
-  }
-  amax = rows4_max(amax);
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  // q times 2^e with |q| 2^e in [2^10, 2^11): the 2^-4 of every second pair
-  // and a small q stay in the normal range
-  const int e = amax > 0.f && amax < INFINITY ? 11 - __builtin_amdgcn_frexp_expf(amax) : 0;
-  const float up = __builtin_amdgcn_ldexpf(1.f, e);
-#pragma unroll
-  for (int s = 0; s < KS; ++s)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      qf[s][i] = static_cast<_Float16>(static_cast<float>(qf[s][i]) * ((i & 2) ? up * 0.0625f : up));
-  const float qk = __builtin_amdgcn_ldexpf(A.qscale, 24 - e);  // score = qk (s_k a + low_k ql)
-  const float ql = __builtin_amdgcn_ldexpf(sum, e - 24);
+  for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const half8*>(qrow + KS * 8 * g + 8 * s);
 
   const int pb = kv4_rows(W.C) * (D / 2);
   uint32_t kx[4][KS], vx[4][KS];
@@ -182,9 +160,9 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
     const int a = g & 1 ? tn[1].*f : tn[0].*f, b = g & 1 ? tn[3].*f : tn[2].*f;
     return g & 2 ? b : a;
   };
-  auto load_words = [&](const char* at, uint32_t (&x)[KS]) {
+  auto load_words = [&](const char* at, uint32_t (&x)[KS], auto nt) {
     if constexpr (D == 128) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(at);
+      const u32x4 a = decltype(nt)::value ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at)) : *reinterpret_cast<const u32x4*>(at);
 #pragma unroll
       for (int s = 0; s < KS; ++s) x[s] = a[s];
     } else {
@@ -195,10 +173,10 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
   };
   int pos_n = 0, end_n = 0;
   int64_t par_n = 0;
+  int lane_off = lane * (D / 8);
   auto load_k = [&]() {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      load_words(W.kbase + tn[t].slot * W.ssb + (tn[t].row + n16) * (D / 2) + g * (D / 8), kx[t]);
+    for (int t = 0; t < 4; ++t) load_words(W.kbase + tn[t].slot * W.ssb + tn[t].row * (D / 2) + lane_off, kx[t], std::true_type{});
     par_n = mine(&Tile::slot) * W.ssb + pb + (mine(&Tile::row) + n16) * 4;
     kp = *reinterpret_cast<const uint32_t*>(W.kbase + par_n);
     pos_n = mine(&Tile::pos) + n16;
@@ -206,10 +184,9 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
   };
   Tile tv[4];
   auto load_v = [&](int64_t par) {
+    vp = *reinterpret_cast<const uint32_t*>(W.vbase + par);  // needed before the codes
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      load_words(W.vbase + tv[t].slot * W.ssb + tv[t].row * (D / 2) + lane * (D / 8), vx[t]);
-    vp = *reinterpret_cast<const uint32_t*>(W.vbase + par);
+    for (int t = 0; t < 4; ++t) load_words(W.vbase + tv[t].slot * W.ssb + tv[t].row * (D / 2) + lane_off, vx[t], std::true_type{});
   };
   auto next = [&](int st) {
     const int steps = (W.n_tiles + 3) / 4;
@@ -233,6 +210,33 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
     for (int t = 0; t < 4; ++t) tv[t] = tn[t];
     load_v(par_n);
   }
+  float amax = 0.f, sum = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = static_cast<float>(qf[s][i]);
+      amax = fmaxf(amax, fabsf(x));
+      sum += x;
+    }
+  amax = rows4_max(amax);
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  // q times 2^e with |q| 2^e in [2^10, 2^11): the 2^-4 of every second pair
+  // and a small q stay in the normal range
+  const int e = amax > 0.f && amax < INFINITY ? 11 - __builtin_amdgcn_frexp_expf(amax) : 0;
+  const float up = __builtin_amdgcn_ldexpf(1.f, e);
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      qf[s][i] = static_cast<_Float16>(static_cast<float>(qf[s][i]) * ((i & 2) ? up * 0.0625f : up));
+  const float qk = __builtin_amdgcn_ldexpf(A.qscale, 24 - e);  // score = qk (s_k a + low_k ql)
+  const float ql = __builtin_amdgcn_ldexpf(sum, e - 24);
+
+  // Every step issues the same loads, so that a wait covers only the rows it
+  // needs (loads under a condition would make each wait one for all of them);
+  // past the last step they are one line of the last tiles each, not used.
   while (st >= 0) {
     floatx4 a[4];
 #pragma unroll
@@ -246,7 +250,8 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
     const half2v kq = __builtin_bit_cast(half2v, kp);
     const int pos = pos_n, end = end_n;
     st = next(st + nw);
-    if (st >= 0) load_k();
+    lane_off = st >= 0 ? lane_off : 0;
+    load_k();
     const bool on = pos < end && pos < W.len && (pos >= W.lo || pos < W.sinks);
     float sc = qk * __builtin_fmaf(raw, static_cast<float>(kq[0]), static_cast<float>(kq[1]) * ql);
     sc = on ? sc : -INFINITY;
@@ -288,11 +293,9 @@ __device__ __forceinline__ void row_kv4(const PlanArgs& A, const Work& W, const 
         acc[2 * s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, pf[r], acc[2 * s], 0, 0, 0);
         acc[2 * s + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, pf[r], acc[2 * s + 1], 0, 0, 0);
       }
-    if (st >= 0) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) tv[t] = tn[t];
-      load_v(par_n);
-    }
+    for (int t = 0; t < 4; ++t) tv[t] = tn[t];
+    load_v(par_n);
   }
   n_run = wave_sum(n_run);
   base = wave_sum(base);
@@ -324,21 +327,25 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
   constexpr int LT = NL / TP;                       // loads of a tile
   constexpr int RB = D * static_cast<int>(sizeof(T));
   const int gi = lane / LPR, li = lane % LPR;
-  float qv[E];
-  Elem<T>::unpack(*reinterpret_cast<const uint4*>(qrow + E * li), qv);
+  const uint4 q_raw = *reinterpret_cast<const uint4*>(qrow + E * li);
   uint4 kx[NL], vx[NL];
   Tile tn[TP], tv[TP];
   auto fetch = [&](int st) {
 #pragma unroll
     for (int t = 0; t < TP; ++t) tn[t] = tile_at(W, TP * st + t);
   };
-  auto load = [&](const char* base, const Tile (&t)[TP], uint4 (&x)[NL]) {
+  int li_off = 16 * li, gi_off = gi;
+  auto load = [&](const char* base, const Tile (&t)[TP], uint4 (&x)[NL], auto nt) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const Tile& y = t[i / LT];
-      // rows past the chunk's size read its last one again
-      const int r = min(y.row + (i % LT) * RPL + gi, W.C - 1);
-      x[i] = *reinterpret_cast<const uint4*>(base + y.slot * W.ssb + static_cast<size_t>(r) * RB + 16 * li);
+      // a scalar base and a small offset of the lane; rows past the chunk's
+      // size read its last one again
+      const char* at = base + y.slot * W.ssb + static_cast<int64_t>(y.row) * RB;
+      const unsigned off = min((i % LT) * RPL + gi_off, W.C - 1 - y.row) * RB + li_off;
+      if constexpr (decltype(nt)::value)
+        x[i] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + off)));
+      else x[i] = *reinterpret_cast<const uint4*>(at + off);
     }
   };
   auto next = [&](int st) {
@@ -358,9 +365,11 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
   for (int j = 0; j < E; ++j) acc[j] = 0.f;
   int st = next(wv);
   if (st >= 0) {
-    load(W.kbase, tn, kx);
-    load(W.vbase, tn, vx);
+    load(W.kbase, tn, kx, std::true_type{});
+    load(W.vbase, tn, vx, std::true_type{});
   }
+  float qv[E];
+  Elem<T>::unpack(q_raw, qv);
   while (st >= 0) {
 #pragma unroll
     for (int t = 0; t < TP; ++t) tv[t] = tn[t];
@@ -374,7 +383,9 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
       sc[i] = group_sum<LPR>(d) * A.qscale;
     }
     st = next(st + nw);
-    if (st >= 0) load(W.kbase, tn, kx);
+    li_off = st >= 0 ? li_off : 0;  // as over 4-bit pools
+    gi_off = st >= 0 ? gi_off : 0;
+    load(W.kbase, tn, kx, std::true_type{});
     bool all = true;
 #pragma unroll
     for (int t = 0; t < TP; ++t) {
@@ -412,7 +423,7 @@ __device__ __forceinline__ void row_plain(const PlanArgs& A, const Work& W, cons
 #pragma unroll
       for (int j = 0; j < E; ++j) acc[j] = __builtin_fmaf(p, x[j], acc[j]);
     }
-    if (st >= 0) load(W.vbase, tn, vx);
+    load(W.vbase, tn, vx, std::true_type{});
   }
 #pragma unroll
   for (int off = LPR; off < 64; off <<= 1) {
@@ -522,16 +533,17 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
     for (int t = 0; t < TP; ++t) {
       const char* kt = W.kbase + tn[t].slot * W.ssb;
       if constexpr (kQ4) {
-        words(kt + (tn[t].row + n16) * (D / 2) + g * (D / 8), kc[t]);
+        words(kt + tn[t].row * (D / 2) + lane * (D / 8), kc[t]);
         kp[t] = *reinterpret_cast<const u32x4*>(kt + pb + (tn[t].row + 4 * g) * 4);
       } else {
-        const char* at = kt + static_cast<size_t>(min(tn[t].row + n16, W.C - 1)) * (D * ES) + 16 * g;
+        const char* at = kt + static_cast<int64_t>(tn[t].row) * (D * ES);
+        const unsigned off = min(n16, W.C - 1 - tn[t].row) * (D * ES) + 16 * g;
         if constexpr (kF16) {
 #pragma unroll
-          for (int s = 0; s < KS; ++s) kh[t][s] = *reinterpret_cast<const half8*>(at + 64 * s);
+          for (int s = 0; s < KS; ++s) kh[t][s] = *reinterpret_cast<const half8*>(at + (off + 64 * s));
         } else {
 #pragma unroll
-          for (int u = 0; u < D / 16; ++u) kf[u] = *reinterpret_cast<const floatx4*>(at + 64 * u);
+          for (int u = 0; u < D / 16; ++u) kf[u] = *reinterpret_cast<const floatx4*>(at + (off + 64 * u));
         }
       }
     }
@@ -541,26 +553,27 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const char* vt = W.vbase + tn[t].slot * W.ssb;
-        words(vt + tn[t].row * (D / 2) + lane * (D / 8), vc[t]);
-        vp[t] = *reinterpret_cast<const u32x4*>(vt + pb + (tn[t].row + 4 * g) * 4);
+        vp[t] = *reinterpret_cast<const u32x4*>(vt + pb + (tn[t].row + 4 * g) * 4);  // needed first
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        words(W.vbase + tn[t].slot * W.ssb + tn[t].row * (D / 2) + lane * (D / 8), vc[t]);
     } else if constexpr (kF16) {
       constexpr int GPR = D / 8, RPL = 64 / GPR;  // granules a row, rows a load
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         const Tile& t = tn[i / (D / 32)];
-        const int r = min(t.row + (i % (D / 32)) * RPL + lane / GPR, W.C - 1);
-        vh[i] = *reinterpret_cast<const u32x4*>(W.vbase + t.slot * W.ssb + static_cast<size_t>(r) * (D * 2) +
-                                                16 * (lane % GPR));
+        const char* at = W.vbase + t.slot * W.ssb + static_cast<int64_t>(t.row) * (D * 2);
+        const unsigned off = min((i % (D / 32)) * RPL + lane / GPR, W.C - 1 - t.row) * (D * 2) + 16 * (lane % GPR);
+        vh[i] = *reinterpret_cast<const u32x4*>(at + off);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = min(tn[0].row + 4 * g + i, W.C - 1);
+        const char* at = W.vbase + tn[0].slot * W.ssb + static_cast<int64_t>(tn[0].row) * (D * 4);
+        const unsigned off = min(4 * g + i, W.C - 1 - tn[0].row) * (D * 4) + 16 * n16;
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u)
-          vf[i][u] = *reinterpret_cast<const floatx4*>(W.vbase + tn[0].slot * W.ssb +
-                                                       static_cast<size_t>(r) * (D * 4) + 256 * u + 16 * n16);
+        for (int u = 0; u < D / 64; ++u) vf[i][u] = *reinterpret_cast<const floatx4*>(at + (off + 256 * u));
       }
     }
   };
@@ -633,7 +646,7 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
       }
     }
     const int st_next = next(st + 4);
-    if (st_next >= 0) load_k();
+    load_k();  // unconditional, as for one row; past the last step, its last tiles again
     float sv[kQ4 ? 2 : 1][4], lv[kQ4 ? 2 : 1][4];
     float smax = 0.f;
     if constexpr (kQ4) {
@@ -749,11 +762,15 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
           n_run += static_cast<float>(pf[4 * t + i]);
         }
       constexpr int GPR = D / 8, RPL = 64 / GPR;
+      bool bad = false;
       if (!all) {
         rare();
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
+        for (int i = 0; i < D / 16; ++i) {
           if (!seen(i / (D / 32), (i % (D / 32)) * RPL + lane / GPR, len_max, lo_min)) vh[i] = u32x4{0, 0, 0, 0};
+          bad |= any_nonfinite(__builtin_bit_cast(half8, vh[i]));
+        }
+        bad = __any(bad);
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
@@ -762,41 +779,45 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
       }
       // the wavefront's own tile: its LDS ops complete in order
       compiler_fence();
-      half8 va[DT];
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
+      auto read_v = [&](int d) {
         const _Float16* at = vl + (4 * g + (n16 >> 2)) * VS + 16 * d + 4 * (n16 & 3);
-        const half4 a = lds_read_tr16(at), b = lds_read_tr16(at + 16 * VS);
-        va[d] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-      compiler_fence();
-      if (!all) {
+        const half4 x = lds_read_tr16(at), y = lds_read_tr16(at + 16 * VS);
+        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      if (bad) {
         rare();
-        bool bad = false;
+        half8 vis;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) bad |= any_nonfinite(va[d]);
-        if (__any(bad)) {
-          half8 vis;
+        for (int k = 0; k < 8; ++k)
+          vis[k] = static_cast<_Float16>(seen(k / 4, 4 * g + k % 4, W.len, W.lo) ? 1.f : 0.f);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            vis[k] = static_cast<_Float16>(seen(k / 4, 4 * g + k % 4, W.len, W.lo) ? 1.f : 0.f);
+        for (int d = 0; d < DT; ++d) {
+          half8 va = read_v(d), x;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            half8 x;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const bool b = !(fabsf(static_cast<float>(va[d][k])) < INFINITY);
-              x[k] = static_cast<_Float16>(b ? 1.f : 0.f);
-              va[d][k] = b ? static_cast<_Float16>(0.f) : va[d][k];
-            }
-            const floatx4 z = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, vis, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[d][i] = z[i] > 0.f ? __builtin_nanf("") : acc[d][i];
+          for (int k = 0; k < 8; ++k) {
+            const bool f = fabsf(static_cast<float>(va[k])) < INFINITY;
+            x[k] = static_cast<_Float16>(f ? 0.f : 1.f);
+            va[k] = f ? va[k] : static_cast<_Float16>(0.f);
           }
+          const floatx4 z = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, vis, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pf, acc[d], 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[d][i] = z[i] > 0.f ? __builtin_nanf("") : acc[d][i];
+        }
+      } else {
+        constexpr int HD = 4;  // operands in registers at once
+#pragma unroll
+        for (int d0 = 0; d0 < DT; d0 += HD) {
+          half8 va[HD];
+#pragma unroll
+          for (int d = 0; d < HD; ++d) va[d] = read_v(d0 + d);
+#pragma unroll
+          for (int d = 0; d < HD; ++d)
+            acc[d0 + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pf, acc[d0 + d], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va[d], pf, acc[d], 0, 0, 0);
+      compiler_fence();
     } else {
       half8 pf, pl;  // P s_v: rounded; what is left, where it has ops of its own
 #pragma unroll
@@ -823,7 +844,7 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
       }
     }
     st = st_next;
-    if (st >= 0) load_v();
+    load_v();
   }
 
   n_run += __shfl_xor(n_run, 16);
@@ -860,7 +881,7 @@ __device__ __forceinline__ void rows_shared(const PlanArgs& A, const Work& W, in
 }
 
 template <int S, int D>
-__global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) void kwd_kernel(PlanArgs A) {
+__global__ __launch_bounds__(256, S == kStoreKv4 ? 3 : 2) void kwd_kernel(PlanArgs A) {
   using T = typename Traits<S>::T;
   constexpr int OS = D + 4;                    // merge buffer row stride (floats)
   constexpr int VB = S == kStoreF16 ? 4 * 32 * (D + 16) * 2 : S == kStoreKv4 ? 4 * 256 : 0;
@@ -894,11 +915,6 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
   Work W;
   // the chunks, one a lane (chunk_stride <= 64)
   W.my = A.chunks[static_cast<size_t>(ib) * A.chunk_stride + min(lane, A.chunk_stride - 1)];
-  // 4-bit, up to 8 rows: columns 8 .. 15 repeat them
-  const int col = S == kStoreKv4 && nr <= 8 ? lane & 7 : lane & 15;
-  const int row = item.row_begin + min(col, nr - 1);
-  const PlanRow prow = A.rows[row];
-  const int io = A.row_map ? A.row_map[row] : row;
   W.kbase = static_cast<const char*>(A.kpool) + h * (A.hs * ES);
   W.vbase = static_cast<const char*>(A.vpool) + h * (A.hs * ES);
   W.ssb = A.ss * ES;
@@ -909,23 +925,39 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 4 : S == kStoreF16 ? 3 : 2) v
   W.n_tiles = item.n_chunks * W.tpc;
   W.sinks = A.sinks;
   W.lo_item = item.lo;
-  W.len = prow.last_start + A.slot_len[prow.last_slot];
-  W.lo = max(0, W.len - A.window);
-  if (tid < kPlanRows) {
-    s_pbase[tid] = prow.pbase;
-    s_np[tid] = prow.np;
-    s_io[tid] = io;
-  }
-  const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
   float* mb = reinterpret_cast<float*>(lds + (S == kStoreKv4 ? VB : 0));  // [wave][row][OS]
   if (nr == 1) {
+    // the row's length is asked for here and waited for where the first
+    // scores are
+    const int io = A.row_map ? A.row_map[item.row_begin] : item.row_begin;
+    W.len = item.last_start + A.slot_len[item.last_slot];
+    W.lo = max(0, W.len - A.window);
+    const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
     float* out = mb + wv * kPlanRows * OS;
     const int w0 = solo ? 0 : wv, nw = solo ? 1 : 4;
     if constexpr (S == kStoreKv4) row_kv4<D>(A, W, qrow, w0, nw, lane, lds + wv * 256, out, &s_m[wv][0], &s_n[wv][0]);
     else row_plain<S, D>(A, W, qrow, w0, nw, lane, out, &s_m[wv][0], &s_n[wv][0]);
+    if (tid == 0) {
+      s_pbase[0] = item.pbase;
+      s_np[0] = item.np;
+      s_io[0] = io;
+    }
   } else {
+    // 4-bit, up to 8 rows: columns 8 .. 15 repeat them
+    const int col = S == kStoreKv4 && nr <= 8 ? lane & 7 : lane & 15;
+    const int row = item.row_begin + min(col, nr - 1);
+    const PlanRow prow = A.rows[row];
+    const int io = A.row_map ? A.row_map[row] : row;
+    const T* qrow = static_cast<const T*>(A.q) + (static_cast<size_t>(io) * H + h) * D;
+    W.len = prow.last_start + A.slot_len[prow.last_slot];
+    W.lo = max(0, W.len - A.window);
     rows_shared<S, D>(A, W, nr, qrow, wv, lane, lds + (S == kStoreF16 ? wv * (32 * (D + 16) * 2) : 0),
                       mb + wv * kPlanRows * OS, s_m[wv], s_n[wv]);
+    if (tid < kPlanRows) {
+      s_pbase[tid] = prow.pbase;
+      s_np[tid] = prow.np;
+      s_io[tid] = io;
+    }
   }
   // Result r of the block: row r of the item, folded from the four wavefronts
   // (Eqn 2) through LDS, [wave][row][channel]; or, of an item of wavefronts,

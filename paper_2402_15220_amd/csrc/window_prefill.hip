@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
         const char* kt = P.kpool + slot * P.ss + h * P.hs;
         const char* vt = P.vpool + slot * P.ss + h * P.hs;
         const int pb = kv4_rows(C) * (D / 2);
-        const char* kc = kt + (row + lane / 4) * (D / 2) + (lane % 4) * (D / 8);
+        const char* kc = kt + row * (D / 2) + lane * (D / 8);
         const char* vc = vt + row * (D / 2) + lane * (D / 8);
         if constexpr (D == 128) {
           kr[i] = *reinterpret_cast<const u32x4*>(kc);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
           kr[i] = u32x4{a[0], a[1], 0, 0};
           vr[i] = u32x4{b[0], b[1], 0, 0};
         }
-        kp[i] = *reinterpret_cast<const uint32_t*>(kt + pb + (row + lane / 4) * 4);
+        kp[i] = *reinterpret_cast<const uint32_t*>(kt + pb + (row + lane % 16) * 4);
         vp[i] = *reinterpret_cast<const u32x4*>(vt + pb + (row + 4 * (lane / 16)) * 4);
       }
     }
@@ -247,8 +247,8 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
       } else {
         const int t0 = i * 4 + wv;
         const int p0 = pick(d.pos, i), e0 = pick(d.end, i);
-        // K: this thread's quarter of row lane / 4
-        const int r = 16 * t0 + lane / 4;
+        // K: this thread's quarter of row lane % 16
+        const int r = 16 * t0 + lane % 16;
         const half2v kpar = __builtin_bit_cast(half2v, kp[i]);
         const half2v ks = {kpar[0], kpar[0]}, ko = {kpar[1], kpar[1]};
 #pragma unroll
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
             y[2 * p] = z[0];
             y[2 * p + 1] = z[1];
           }
-          const int c = (lane % 4) * CW + w;  // granule of the row
+          const int c = (lane / 16) * CW + w;  // granule of the row
           *reinterpret_cast<half8*>(kl + r * (D * 2) + 16 * (c ^ swz<D>(r))) = y;
         }
         // V: tokens 4g .. 4g + 3 of the tile at channels 32 w + 16 b + n, to

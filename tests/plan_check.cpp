@@ -33,6 +33,12 @@ static int check(const ChunkTree& tree, const Plan& P, int window, int sinks, co
     if (it.n_rows < 1 || it.n_rows > kPlanRows || it.n_chunks < 1 || it.n_chunks > P.stride ||
         P.stride > kPlanChunks || it.row_begin < 0 || it.row_begin + it.n_rows > B)
       return std::printf("%s: item %zu\n", what, i), 1;
+    if (it.n_rows == 1 && !(P.first_item[it.row_begin] >= 0 && static_cast<int>(i) >= P.first_item[it.row_begin] &&
+                            static_cast<int>(i) <= P.last_item[it.row_begin] &&
+                            it.last_slot == P.rows[it.row_begin].last_slot &&
+                            it.last_start == P.rows[it.row_begin].last_start && it.pbase == P.rows[it.row_begin].pbase &&
+                            it.np == P.rows[it.row_begin].np))
+      return std::printf("%s: row of item %zu\n", what, i), 1;
     for (int r = it.row_begin; r < it.row_begin + it.n_rows; ++r) {
       if (!ords[r].insert(it.ord).second) return std::printf("%s: ord twice\n", what), 1;
       const long lo = len[r] > window ? len[r] - window : 0;
@@ -88,7 +94,7 @@ int main() {
       Tables t;
       build_tables(tree, &t);
       Plan P;
-      build_plan(tree, t, window, sinks, in(1, 32), 256, &P);
+      build_plan(tree, t, window, sinks, in(1, 32), 256, in(1, 16), &P);
       std::unordered_map<int64_t, int32_t> row_of;
       for (size_t r = 0; r < t.row_seq.size(); ++r) row_of[t.row_seq[r]] = static_cast<int32_t>(r);
       tree.clear_dirty();

@@ -72,15 +72,15 @@ def kv4_prefill_slack(tree, sid, q, window, sinks, scale):
 
 
 def unpack_tile(tile, C, D):
-    """Codes [rows, D], scale and low [rows] of one (slot, head) tile of a 4-bit
-    pool: K tiles token-major, V tiles in the transposed order (both returned
-    as (k view, v view) by the caller's choice of `order`)."""
+    """Of one (slot, head) tile of a 4-bit pool: its codes [rows, D] read as a K
+    tile and as a V tile, scale and low [rows]."""
     rows = -(-C // 16) * 16
     words = tile[: rows * D // 2].view(np.uint32)
     par = tile[rows * D // 2: rows * (D // 2 + 4)].view(np.float16).reshape(rows, 2)
     nib = np.array([(k >> 1) + 4 * (k & 1) for k in range(8)])
     k8 = (words[:, None] >> (4 * nib)[None, :]) & 15          # element k of every word
-    k_codes = k8.reshape(rows, D).astype(np.uint8)
+    # K: block, group g, token n, word w of the group: elements 8 (g D/32 + w) ..
+    k_codes = k8.reshape(rows // 16, 4, 16, D // 32, 8).transpose(0, 2, 1, 3, 4).reshape(rows, D).astype(np.uint8)
     # V: block, group g, channel n, tile pair t; element 4 b + i is token 4 g + i, channel 32 t + 16 b + n
     v = k8.reshape(rows // 16, 4, 16, D // 32, 2, 4)
     v_codes = v.transpose(0, 1, 5, 3, 4, 2).reshape(rows, D).astype(np.uint8)
