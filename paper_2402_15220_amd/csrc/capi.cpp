@@ -1083,16 +1083,14 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   a.sinks = sinks;
   a.qscale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(a.D)) : scale) * 1.4426950408889634f;
 
-  // 128-query tiles where they give every compute unit a block, else 64-query
-  // ones, whose keys are cut into parts of at least four units while two
-  // blocks a compute unit are not there.
   const int64_t cus = cache->num_cus;
-  a.tile_rows = (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
+  a.tile_rows = cache->kv4() ? (n_q > 64 && !getenv("CA_T64") ? 128 : 64) : (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
   const int64_t tiles = (n_q + a.tile_rows - 1) / a.tile_rows * a.H;
   const int64_t units = (std::min<int64_t>(L, std::min<int64_t>(L, window) + a.tile_rows) +
                          std::min<int64_t>(L, sinks)) / 64;
-  if (a.tile_rows == 64)
-    a.n_split = static_cast<int>(std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>(2 * cus / tiles, units / 4))));
+  const int64_t minu = getenv("CA_MU") ? atoi(getenv("CA_MU")) : 2;
+  if (a.tile_rows == 64 || cache->kv4())
+    a.n_split = static_cast<int>(std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>((getenv("CA_BL")?atoi(getenv("CA_BL")):2) * cus / tiles, units / minu))));
   const size_t ws = a.n_split > 1 ? static_cast<size_t>(tiles) * a.n_split *
                                         ca::window_prefill_part_bytes(a.tile_rows, a.D)
                                   : 0;
@@ -1123,6 +1121,13 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
     a.ws_bytes = ws;
     a.cnt = cache->d_pf_cnt;
     a.cnt_shift = ca::tile_counter_shift(static_cast<size_t>(tiles));
+  }
+  if (a.store == ca::kStoreKv4) {
+    ca::Kv4PrefillArgs b{a.H, a.D, a.C, a.q, a.o, a.kpool, a.vpool, a.ss, a.hs, a.host_path, a.path, a.n_chunks,
+                         a.n_q, a.L, a.window, a.sinks, a.qscale, a.tile_rows, a.n_split, a.ws, a.ws_bytes, a.cnt, a.cnt_shift};
+    const hipError_t e = ca::launch_kv4_prefill(b, s);
+    if (e != hipSuccess) return hip_fail(e, "prefill launch");
+    return CA_OK;
   }
   const hipError_t e = ca::launch_window_prefill(a, s);
   if (e != hipSuccess) return hip_fail(e, "prefill launch");

@@ -181,6 +181,34 @@ struct PlanArgs {
 };
 hipError_t launch_plan_attention(const PlanArgs& a, hipStream_t stream);
 
+// Prefill attention over a 4-bit pool, with or without a sliding window and
+// sinks (kv4_prefill.hip).
+struct Kv4PrefillArgs {
+  int H, D, C;
+  const void* q;
+  void* o;
+  const void* kpool;
+  const void* vpool;
+  int64_t ss, hs;  // pool strides of a slot and of a head (bytes)
+  // the chunks that some query sees, root -> leaf: slots, starts, ends, n_chunks
+  // each; on the host (up to kPrefillInlineChunks) or on the device
+  const int32_t* host_path;
+  const int32_t* path;
+  int n_chunks;
+  int n_q;
+  int L;  // positions of the sequence
+  int window, sinks;
+  float qscale;
+  int tile_rows;    // queries of a block's tile: 128 or 64
+  int n_split = 1;  // parts of a tile's keys, in blocks of their own
+  float* ws = nullptr;  // n_split > 1: kv4_prefill_part_bytes() per tile and part
+  size_t ws_bytes = 0;
+  int32_t* cnt = nullptr;  // n_split > 1: a zeroed counter per tile, left at zero
+  int cnt_shift = 0;
+};
+constexpr size_t kv4_prefill_part_bytes(int rows, int D) { return static_cast<size_t>(rows) * (D + 2) * 4; }
+hipError_t launch_kv4_prefill(const Kv4PrefillArgs& a, hipStream_t stream);
+
 // Prefill attention with a sliding window and sinks over an fp16 or a 4-bit
 // pool, and every prefill call over a 4-bit one (window_prefill.hip).
 struct WindowPrefillArgs {
