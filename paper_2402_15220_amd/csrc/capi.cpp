@@ -1084,13 +1084,20 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   a.qscale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(a.D)) : scale) * 1.4426950408889634f;
 
   const int64_t cus = cache->num_cus;
-  a.tile_rows = cache->kv4() ? (n_q > 64 && !getenv("CA_T64") ? 128 : 64) : (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
+  // Tiles of 128 queries once they give every CU a block: they read each key for
+  // twice the queries of a 64-query tile. Below that, tiles of 64 and parts of
+  // the keys. Over 4 bits the 128-query blocks are four wavefronts (two blocks a
+  // CU, so twice the parts), the 64-query ones eight: with a window of 1,024 and
+  // 32 heads of 128, tiles of 64 and of 128 take 64 and 59 us at 1,024 queries, 124
+  // and 74 at 2,048; at 512 tiles of 64 in blocks of four and of eight wavefronts
+  // take 39 and 33. A part is at least two units of keys.
+  a.tile_rows = (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
   const int64_t tiles = (n_q + a.tile_rows - 1) / a.tile_rows * a.H;
-  const int64_t units = (std::min<int64_t>(L, std::min<int64_t>(L, window) + a.tile_rows) +
-                         std::min<int64_t>(L, sinks)) / 64;
-  const int64_t minu = getenv("CA_MU") ? atoi(getenv("CA_MU")) : 2;
-  if (a.tile_rows == 64 || cache->kv4())
-    a.n_split = static_cast<int>(std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>((getenv("CA_BL")?atoi(getenv("CA_BL")):2) * cus / tiles, units / minu))));
+  const int64_t keys = std::min<int64_t>(L, std::min<int64_t>(L, window) + a.tile_rows) + std::min<int64_t>(L, sinks);
+  const bool wide = cache->kv4() && a.tile_rows == 64;  // units of 128 keys, one block a CU
+  if (cache->kv4() || a.tile_rows == 64)
+    a.n_split = static_cast<int>(std::min<int64_t>(
+        16, std::max<int64_t>(1, std::min<int64_t>((wide ? 1 : 2) * cus / tiles, keys / (wide ? 256 : 128)))));
   const size_t ws = a.n_split > 1 ? static_cast<size_t>(tiles) * a.n_split *
                                         ca::window_prefill_part_bytes(a.tile_rows, a.D)
                                   : 0;

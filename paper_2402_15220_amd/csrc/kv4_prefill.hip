@@ -4,7 +4,7 @@
 // The last n_q tokens of a sequence of L tokens attend causally: the query at
 // position p sees the positions j <= p with j < sinks or j > p - window.
 //
-// One block of four wavefronts per (tile of 32 QW queries, head, part of the
+// One block of QW KG wavefronts per (tile of 32 QW queries, head, part of the
 // tile's keys). The keys that some query of the tile sees are taken as tiles
 // of 16 rows of the path's chunks, in order, UK / 16 of them to a unit; tiles
 // between the sinks and the first query's window are left out. Codes go from
@@ -111,12 +111,12 @@ __device__ __forceinline__ RowPar row_par(uint32_t w) {
 }
 
 template <int D, int QW, int KG, int KPW, bool INL>
-__global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
-                                                     const std::conditional_t<INL, KwpPath, KwpNoPath> path) {
-  static_assert(QW * KG == 4, "four wavefronts");
+__global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
+    KwpParams P, const std::conditional_t<INL, KwpPath, KwpNoPath> path) {
+  constexpr int NT = 64 * QW * KG;     // threads
   constexpr int QR = 32 * QW;          // queries of a tile
   constexpr int UK = KG * KPW;         // keys of a unit
-  static_assert(UK == 64, "a tile of a unit to each wavefront's load");
+  static_assert(UK == 16 * QW * KG, "a tile of a unit to each wavefront");
   constexpr int ST = UK / 16;          // 16-row tiles of a unit
   constexpr int KS = D / 16;           // 32x32x16 steps over d
   constexpr int DT = D / 32;           // 32-channel tiles of O^T
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
   if (!s_last) return;
   // four parts of four places (row, four channels) a thread, all their loads in
   // flight together: one after the other, the round trips took 30 us here
-  constexpr int IPT = QR * (D / 4) / 256, NI = 4, NB = 4;
+  constexpr int IPT = QR * (D / 4) / NT, NI = IPT < 4 ? IPT : 4, NB = 4;
   static_assert(IPT % NI == 0, "places of a thread");
   const int rows = min(QR, n_q - q0);
 #pragma unroll 1
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
         const uint32_t at = (static_cast<uint32_t>(vt) * P.n_split + min(p0 + p, P.n_split - 1)) * kPart;
 #pragma unroll
         for (int k = 0; k < NI; ++k) {
-          const int i = tid + 256 * (k0 + k), row = i / (D / 4), ch = 4 * (i % (D / 4));
+          const int i = tid + NT * (k0 + k), row = i / (D / 4), ch = 4 * (i % (D / 4));
           const float* ml = P.ws + at / 4 + QR * D + 2 * row;
           pm[p][k] = ld_dev(ml);
           pn[p][k] = ld_dev(ml + 1);
@@ -638,7 +638,7 @@ __global__ __launch_bounds__(256, 2) void kwp_kernel(KwpParams P,
     }
 #pragma unroll
     for (int k = 0; k < NI; ++k) {
-      const int i = tid + 256 * (k0 + k), row = i / (D / 4), ch = 4 * (i % (D / 4));
+      const int i = tid + NT * (k0 + k), row = i / (D / 4), ch = 4 * (i % (D / 4));
       if (row < rows) write4(row, ch, x[k], 1.f / n[k]);
     }
   }
@@ -655,9 +655,9 @@ void launch_wp(const KwpParams& P, const Kv4PrefillArgs& a, hipStream_t stream) 
       path.start[j] = a.host_path[a.n_chunks + j];
       path.end[j] = a.host_path[2 * a.n_chunks + j];
     }
-    kwp_kernel<D, QW, KG, KPW, true><<<grid, 256, 0, stream>>>(P, path);
+    kwp_kernel<D, QW, KG, KPW, true><<<grid, 64 * QW * KG, 0, stream>>>(P, path);
   } else {
-    kwp_kernel<D, QW, KG, KPW, false><<<grid, 256, 0, stream>>>(P, KwpNoPath{});
+    kwp_kernel<D, QW, KG, KPW, false><<<grid, 64 * QW * KG, 0, stream>>>(P, KwpNoPath{});
   }
 }
 
@@ -673,9 +673,9 @@ hipError_t launch_kv4_prefill(const Kv4PrefillArgs& a, hipStream_t stream) {
                     a.path, a.n_chunks, a.n_q, a.H, a.C, a.L, a.window, a.sinks, a.qscale, a.n_split, a.ws,
                     a.cnt, a.cnt_shift, static_cast<uint32_t>(a.ws_bytes)};
   if (a.D == 128 && a.tile_rows == 128) launch_wp<128, 4, 1, 64>(P, a, stream);
-  else if (a.D == 128 && a.tile_rows == 64) launch_wp<128, 2, 2, 32>(P, a, stream);
+  else if (a.D == 128 && a.tile_rows == 64) launch_wp<128, 2, 4, 32>(P, a, stream);
   else if (a.D == 64 && a.tile_rows == 128) launch_wp<64, 4, 1, 64>(P, a, stream);
-  else if (a.D == 64 && a.tile_rows == 64) launch_wp<64, 2, 2, 32>(P, a, stream);
+  else if (a.D == 64 && a.tile_rows == 64) launch_wp<64, 2, 4, 32>(P, a, stream);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
