@@ -37,8 +37,7 @@ SANITIZE = ("-Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined "
             "-Xarch_host -fno-omit-frame-pointer -Xarch_host -g -shared-libasan").split()
 
 SOURCES = ["tree.cpp", "tables.cpp", "plan.cpp", "capi.cpp", "kernels.hip", "prefill.hip",
-           "window.hip", "window_prefill.hip", "kv4.hip",
-           "kv4_prefill.hip", "fill.hip", "scratch.hip"]
+           "window.hip", "kv4.hip", "kv4_prefill.hip", "fill.hip", "scratch.hip"]
 
 
 def _compile(src: str, objdir: str, extra: list) -> str:

@@ -1022,8 +1022,93 @@ ca_status ca_prepare(ca_cache* cache, void* stream, int32_t* uploaded) try {
   return on_exception("ca_prepare");
 }
 
-// Prefill over the 16-row tiles of a path (window_prefill.hip): what a query
-// sees may be a window, and the pool fp16 or 4-bit.
+// Tile and parts of an fp16 prefill: n_q queries over up to nc chunks each, the
+// tiles' keys between `shortest` and `longest` in number. Returns the parts, and
+// in *tile_rows the queries of a tile of 32-query wavefronts (0: 16-query ones).
+static int64_t prefill_shape(const ca_cache* cache, int64_t n_q, int64_t nc, int64_t shortest, int64_t longest,
+                             int* tile_rows) {
+  const int H = cache->cfg.num_heads, D = cache->cfg.head_dim, C = cache->cfg.chunk_size;
+  *tile_rows = 0;
+  // Key-range split of the 16-query blocks: when the (64-query tile, head)
+  // blocks alone would leave compute units idle, cut each tile's units (64-row
+  // pieces of its chunks) into parts of at least six units, run by separate
+  // blocks. One block fits a compute unit, so more blocks than those run in
+  // rounds; a block takes a fixed ~5 us (start, first loads, merge, stores)
+  // and ~1.6 us per pair of units, a split ~1.5 us more and ~0.35 us per part
+  // for the fold. The part count is the one that model finds fastest (32
+  // heads, 1 / 2 / 3 / 4 parts: 130 queries over 1,154 positions 19.3 / 15.7 /
+  // 22.3 / 25.3 us, 300 over 1,324 22.4 / 30.6 / 27.2 / 37.3, 300 over 4,300
+  // 58.1 / 64.8 / 53.7 / 65.9; rounding the parts up to a block per compute
+  // unit took 22.7, 31.1 and 66.9). It is a fit for choosing between rounds, inside
+  // the limit of six units a part: there it is within 4% of the best count timed;
+  // beyond, it would ask for more parts than pay (64 queries over 1,536 positions,
+  // 4 / 6 / 8 parts: 12.7 / 11.8 / 12.5 by the model, 13.7 / 13.7 / 14.1 measured).
+  const int64_t tiles = (n_q + 63) / 64 * static_cast<int64_t>(H);
+  const int64_t units = static_cast<int64_t>(nc) * ((C + 63) / 64);
+  int64_t split = 1;
+  const int64_t cus = cache->num_cus;
+  double best_us = 0;
+  if (cache->prefill_split > 0) {
+    split = cache->prefill_split;
+  } else {
+    const int64_t most = tiles < cus ? std::min<int64_t>(std::max<int64_t>(1, units / 6), 16) : 1;
+    for (int64_t k = 1; k <= most; ++k) {
+      const int64_t rounds = (tiles * k + cus - 1) / cus;
+      const int64_t pairs = (units + 2 * k - 1) / (2 * k);
+      const double us = rounds * (5.0 + 1.6 * pairs) + (k > 1 ? 1.5 + 0.35 * k : 0.0);
+      if (k == 1 || us < best_us) {
+        best_us = us;
+        split = k;
+      }
+    }
+  }
+  // 32-query wavefronts where the 16-query blocks would need a second round:
+  // 128-query tiles where those give every compute unit a block (each K/V
+  // element through the caches once per 128 queries), else 64-query ones. Up to
+  // a block per compute unit the 16-query blocks and their key-range split
+  // stay. 32 heads, 16-query / 64 / 128-query blocks: 1,100 queries over 1,100
+  // positions 36.4 / 26.0 / 27.0 us, 900 over 1,200 37.8 / 27.5 / 26.6, 576 over
+  // 4,000 97.7 / 67.1 / 67.0, 513 over 1,536 40.8 / 28.3 / 29.8; 512 over 1,536
+  // 24.7 / 25.0 / 29.8, over 512 11.5 / 12.3 / 14.1, over 6,000 82.0 / 80.0 / 98.5;
+  // 300 over 300 9.0 / 9.5 / 10.3.
+  // At d = 64 a tile has half the work per unit. Up to 128-query tiles for every
+  // compute unit the 16-query blocks stay (16 heads, 1,024 over 2,024 20.4 / 22.5
+  // us); above, 128-query tiles pay where they come in rounds enough to even out
+  // (8,155 over 8,155 248 / 203 / 194, 32 heads, 4,059 over 4,059 137 in 16-query,
+  // 110 in 128-query tiles) or are of like lengths, behind a cached prefix (32
+  // heads, 2,011 over 6,033 154 / 133 / 125; but 987 over 2,961, 256 tiles, 42 /
+  // 41 / 40); else their longest tile sets the time and 64-query ones do better
+  // (10 heads, 3,400 over 3,400 43.5 / 43.7 / 58.7, 8 heads, 4,059 over 4,059 45.9
+  // in 16-query, 51.2 in 128-query tiles). Chunks of 33 to 63 tokens leave the
+  // 128-query tiles' 64-row units part masked, and few tiles lose to the 16-query
+  // blocks either way (48-token chunks, 32 heads, 1,499 over 1,499 48.9 / 39.2 /
+  // 53.2, 987 over 987 25.8 / 27.9 / 26.8).
+  // Over chunks of at most 32 tokens the 64-query tiles go wherever they are
+  // the faster by the same kind of model (two blocks a compute unit, ~0.87 us
+  // per pair of 32-row units, which hold two 16-token chunks; 300 queries over
+  // 1,300 positions in 16-token chunks: 80 us in one part of 16-query blocks,
+  // 65 in three, 23 so), but not for one or two chunks, which a 16-query block
+  // takes in one pair (2 heads, 16 queries over 16 positions in 16-token chunks 4.7
+  // us in 16-query blocks / 5.5 in 64-query tiles, 32 over 32 5.6 / 5.9, 48 over 48
+  // 7.3 / 6.3).
+  if (cache->prefill_split <= 1) {
+    const int64_t units32 = C == 16 ? (nc + 1) / 2 : static_cast<int64_t>(nc) * ((C + 31) / 32);
+    const double us64 = (tiles + 2 * cus - 1) / (2 * cus) * (5.0 + 0.87 * ((units32 + 1) / 2));
+    const int64_t tiles128 = (n_q + 127) / 128 * H;
+    // d = 64: rounds enough, or at least 2/7 of the path cached; units filled
+    const bool even = tiles128 >= 3 * cus || (4 * tiles128 >= 7 * cus && 7 * shortest >= 2 * longest);
+    const bool filled = C >= 64 || C == 32 || C == 16;
+    if (tiles128 >= cus && (D == 128 || (even && filled))) *tile_rows = 128;
+    else if (C <= 32 ? cache->prefill_split == 0 && nc > 2 && us64 < best_us
+             : D == 128 ? tiles > cus
+                        : tiles128 >= cus && (filled || 2 * tiles128 >= 3 * cus))
+      *tile_rows = 64;
+    if (*tile_rows > 0) split = 1;
+  }
+  return split;
+}
+
+// Prefill where what a query sees may be a window, and the pool fp16 or 4-bit.
 static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void* q, void* o, int64_t n_q,
                                      int32_t window, int32_t sinks, float scale, void* stream,
                                      const char* what) {
@@ -1065,79 +1150,97 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   hp.insert(hp.end(), starts.begin(), starts.end());
   hp.insert(hp.end(), ends.begin(), ends.end());
 
-  ca::WindowPrefillArgs a{};
-  a.store = cache->kv4() ? ca::kStoreKv4 : ca::kStoreF16;
-  a.H = cache->cfg.num_heads;
-  a.D = cache->cfg.head_dim;
-  a.C = cache->cfg.chunk_size;
-  a.q = q;
-  a.o = o;
-  a.kpool = cache->cfg.k_pool;
-  a.vpool = cache->cfg.v_pool;
-  a.ss = cache->cfg.slot_stride;
-  a.hs = cache->cfg.head_stride;
-  a.n_chunks = nc;
-  a.n_q = static_cast<int>(n_q);
-  a.L = static_cast<int>(L);
-  a.window = window;
-  a.sinks = sinks;
-  a.qscale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(a.D)) : scale) * 1.4426950408889634f;
-
-  const int64_t cus = cache->num_cus;
-  // Tiles of 128 queries once they give every CU a block: they read each key for
-  // twice the queries of a 64-query tile. Below that, tiles of 64 and parts of
-  // the keys. Over 4 bits the 128-query blocks are four wavefronts (two blocks a
-  // CU, so twice the parts), the 64-query ones eight: with a window of 1,024 and
-  // 32 heads of 128, tiles of 64 and of 128 take 64 and 59 us at 1,024 queries, 124
-  // and 74 at 2,048; at 512 tiles of 64 in blocks of four and of eight wavefronts
-  // take 39 and 33. A part is at least two units of keys.
-  a.tile_rows = (n_q + 127) / 128 * a.H >= cus ? 128 : 64;
-  const int64_t tiles = (n_q + a.tile_rows - 1) / a.tile_rows * a.H;
-  const int64_t keys = std::min<int64_t>(L, std::min<int64_t>(L, window) + a.tile_rows) + std::min<int64_t>(L, sinks);
-  const bool wide = cache->kv4() && a.tile_rows == 64;  // units of 128 keys, one block a CU
-  if (cache->kv4() || a.tile_rows == 64)
-    a.n_split = static_cast<int>(std::min<int64_t>(
-        16, std::max<int64_t>(1, std::min<int64_t>((wide ? 1 : 2) * cus / tiles, keys / (wide ? 256 : 128)))));
-  const size_t ws = a.n_split > 1 ? static_cast<size_t>(tiles) * a.n_split *
-                                        ca::window_prefill_part_bytes(a.tile_rows, a.D)
-                                  : 0;
-  const size_t counters = a.n_split > 1 ? static_cast<size_t>(tiles) << ca::tile_counter_shift(static_cast<size_t>(tiles)) : 0;
+  const int H = cache->cfg.num_heads, D = cache->cfg.head_dim, C = cache->cfg.chunk_size;
+  const float qscale = (scale == 0.f ? 1.f / std::sqrt(static_cast<float>(D)) : scale) * 1.4426950408889634f;
+  const int64_t seen = std::min<int64_t>(L, window), first = std::min<int64_t>(L, sinks);
+  int tile_rows = 0;  // of a block; 0: 64, by 16-query wavefronts
+  int64_t n_split = 1;
+  if (cache->kv4()) {
+    // Tiles of 128 queries once they give every CU a block: they read each key for
+    // twice the queries of a 64-query tile. Below that, tiles of 64 and parts of
+    // the keys. The 128-query blocks are four wavefronts (two blocks a CU, so
+    // twice the parts), the 64-query ones eight: with a window of 1,024 and 32
+    // heads of 128, tiles of 64 and of 128 take 64 and 59 us at 1,024 queries, 124
+    // and 74 at 2,048; at 512 tiles of 64 in blocks of four and of eight wavefronts
+    // take 39 and 33. A part is at least two units of keys.
+    const int64_t cus = cache->num_cus;
+    tile_rows = (n_q + 127) / 128 * H >= cus ? 128 : 64;
+    const int64_t blocks = (n_q + tile_rows - 1) / tile_rows * H;
+    const int64_t keys = std::min<int64_t>(L, seen + tile_rows) + first;
+    const bool wide = tile_rows == 64;  // units of 128 keys, one block a CU
+    n_split = std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>((wide ? 1 : 2) * cus / blocks,
+                                                                          keys / (wide ? 256 : 128))));
+  } else {
+    // a 64-query tile sees so many chunks at most
+    const int64_t most = (seen + 64 + C - 1) / C + 1 + (first + C - 1) / C;
+    n_split = prefill_shape(cache, n_q, std::min<int64_t>(nc, most), std::min<int64_t>(L - n_q, seen), seen, &tile_rows);
+  }
+  const int rows = tile_rows == 128 ? 128 : 64;
+  const int64_t tiles = (n_q + rows - 1) / rows * H;
+  const size_t ws =
+      n_split > 1 ? static_cast<size_t>(tiles * n_split) * ca::kv4_prefill_part_bytes(rows, D) : 0;
+  const int cnt_shift = ca::tile_counter_shift(static_cast<size_t>(tiles));
+  const size_t counters = n_split > 1 ? static_cast<size_t>(tiles) << cnt_shift : 0;
   const size_t path_bytes = hp.size() * sizeof(int32_t);
   const bool inline_path = nc <= ca::kPrefillInlineChunks;
   if ((!inline_path || ws > cache->d_pf_ws_cap || counters > cache->d_pf_cnt_cap) && capturing(s))
     return fail(CA_ERR_INVALID, std::string(what) + ": a call that is being captured can neither copy a "
                                                     "long path nor grow the partials' memory");
-  if (inline_path) {
-    a.host_path = hp.data();
-  } else {
+  const int32_t* dpath = nullptr;
+  if (!inline_path) {
     char* h = nullptr;
     if ((st = cache->prefill_stage.acquire(path_bytes, &h)) != CA_OK) return st;
     std::memcpy(h, hp.data(), path_bytes);
     if ((st = ensure_device(&cache->d_path, &cache->d_path_cap, path_bytes, s, "prefill path")) != CA_OK)
       return st;
     if ((st = cache->prefill_stage.copy(cache->d_path, path_bytes, s)) != CA_OK) return st;
-    a.path = reinterpret_cast<const int32_t*>(cache->d_path);
+    dpath = reinterpret_cast<const int32_t*>(cache->d_path);
   }
-  if (a.n_split > 1) {
+  if (n_split > 1) {
     if ((st = ensure_device(reinterpret_cast<char**>(&cache->d_pf_ws), &cache->d_pf_ws_cap, ws, s,
                             "prefill partials")) != CA_OK)
       return st;
     if ((st = ca_cache::ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap, counters, s)) != CA_OK)
       return st;
-    a.ws = cache->d_pf_ws;
+  }
+  auto common = [&](auto& a) {
+    a.H = H;
+    a.D = D;
+    a.C = C;
+    a.q = q;
+    a.o = o;
+    a.kpool = cache->cfg.k_pool;
+    a.vpool = cache->cfg.v_pool;
+    a.ss = cache->cfg.slot_stride;
+    a.hs = cache->cfg.head_stride;
+    a.host_path = inline_path ? hp.data() : nullptr;
+    a.n_chunks = nc;
+    a.n_q = static_cast<int>(n_q);
+    a.L = static_cast<int>(L);
+    a.window = window;
+    a.sinks = sinks;
+    a.qscale = qscale;
+    a.tile_rows = tile_rows;
+    a.n_split = static_cast<int>(n_split);
+    a.ws = n_split > 1 ? cache->d_pf_ws : nullptr;
     a.ws_bytes = ws;
-    a.cnt = cache->d_pf_cnt;
-    a.cnt_shift = ca::tile_counter_shift(static_cast<size_t>(tiles));
+    a.cnt = n_split > 1 ? cache->d_pf_cnt : nullptr;
+    a.cnt_shift = cnt_shift;
+  };
+  hipError_t e;
+  if (cache->kv4()) {
+    ca::Kv4PrefillArgs a{};
+    common(a);
+    a.path = dpath;
+    e = ca::launch_kv4_prefill(a, s);
+  } else {
+    ca::PrefillArgs a{};
+    common(a);
+    a.chunk_slot = dpath;
+    a.chunk_start = dpath ? dpath + nc : nullptr;
+    e = ca::launch_prefill(a, s);
   }
-  if (a.store == ca::kStoreKv4) {
-    ca::Kv4PrefillArgs b{a.H, a.D, a.C, a.q, a.o, a.kpool, a.vpool, a.ss, a.hs, a.host_path, a.path, a.n_chunks,
-                         a.n_q, a.L, a.window, a.sinks, a.qscale, a.tile_rows, a.n_split, a.ws, a.ws_bytes, a.cnt, a.cnt_shift};
-    const hipError_t e = ca::launch_kv4_prefill(b, s);
-    if (e != hipSuccess) return hip_fail(e, "prefill launch");
-    return CA_OK;
-  }
-  const hipError_t e = ca::launch_window_prefill(a, s);
-  if (e != hipSuccess) return hip_fail(e, "prefill launch");
+  if (e != hipSuccess) return hip_fail(e, what);
   return CA_OK;
 }
 
@@ -1232,84 +1335,10 @@ ca_status ca_prefill_attention(ca_cache* cache, int64_t seq_id, const void* q, v
   a.L = pos;
   const float sc = scale == 0.f ? 1.f / std::sqrt(static_cast<float>(a.D)) : scale;
   a.qscale = sc * 1.4426950408889634f;
-  // Key-range split of the 16-query blocks: when the (64-query tile, head)
-  // blocks alone would leave compute units idle, cut each tile's units (64-row
-  // pieces of its chunks) into parts of at least six units, run by separate
-  // blocks. One block fits a compute unit, so more blocks than those run in
-  // rounds; a block takes a fixed ~5 us (start, first loads, merge, stores)
-  // and ~1.6 us per pair of units, a split ~1.5 us more and ~0.35 us per part
-  // for the fold. The part count is the one that model finds fastest (32
-  // heads, 1 / 2 / 3 / 4 parts: 130 queries over 1,154 positions 19.3 / 15.7 /
-  // 22.3 / 25.3 us, 300 over 1,324 22.4 / 30.6 / 27.2 / 37.3, 300 over 4,300
-  // 58.1 / 64.8 / 53.7 / 65.9; rounding the parts up to a block per compute
-  // unit took 22.7, 31.1 and 66.9). It is a fit for choosing between rounds, inside
-  // the limit of six units a part: there it is within 4% of the best count timed;
-  // beyond, it would ask for more parts than pay (64 queries over 1,536 positions,
-  // 4 / 6 / 8 parts: 12.7 / 11.8 / 12.5 by the model, 13.7 / 13.7 / 14.1 measured).
-  const int64_t tiles = (n_q + 63) / 64 * static_cast<int64_t>(a.H);
-  const int64_t units = static_cast<int64_t>(nc) * ((a.C + 63) / 64);
-  int64_t split = 1;
-  const int64_t cus = cache->num_cus;
-  double best_us = 0;
-  if (cache->prefill_split > 0) {
-    split = cache->prefill_split;
-  } else {
-    const int64_t most = tiles < cus ? std::min<int64_t>(std::max<int64_t>(1, units / 6), 16) : 1;
-    for (int64_t k = 1; k <= most; ++k) {
-      const int64_t rounds = (tiles * k + cus - 1) / cus;
-      const int64_t pairs = (units + 2 * k - 1) / (2 * k);
-      const double us = rounds * (5.0 + 1.6 * pairs) + (k > 1 ? 1.5 + 0.35 * k : 0.0);
-      if (k == 1 || us < best_us) {
-        best_us = us;
-        split = k;
-      }
-    }
-  }
-  // 32-query wavefronts where the 16-query blocks would need a second round:
-  // 128-query tiles where those give every compute unit a block (each K/V
-  // element through the caches once per 128 queries), else 64-query ones. Up to
-  // a block per compute unit the 16-query blocks and their key-range split
-  // stay. 32 heads, 16-query / 64 / 128-query blocks: 1,100 queries over 1,100
-  // positions 36.4 / 26.0 / 27.0 us, 900 over 1,200 37.8 / 27.5 / 26.6, 576 over
-  // 4,000 97.7 / 67.1 / 67.0, 513 over 1,536 40.8 / 28.3 / 29.8; 512 over 1,536
-  // 24.7 / 25.0 / 29.8, over 512 11.5 / 12.3 / 14.1, over 6,000 82.0 / 80.0 / 98.5;
-  // 300 over 300 9.0 / 9.5 / 10.3.
-  // At d = 64 a tile has half the work per unit. Up to 128-query tiles for every
-  // compute unit the 16-query blocks stay (16 heads, 1,024 over 2,024 20.4 / 22.5
-  // us); above, 128-query tiles pay where they come in rounds enough to even out
-  // (8,155 over 8,155 248 / 203 / 194, 32 heads, 4,059 over 4,059 137 in 16-query,
-  // 110 in 128-query tiles) or are of like lengths, behind a cached prefix (32
-  // heads, 2,011 over 6,033 154 / 133 / 125; but 987 over 2,961, 256 tiles, 42 /
-  // 41 / 40); else their longest tile sets the time and 64-query ones do better
-  // (10 heads, 3,400 over 3,400 43.5 / 43.7 / 58.7, 8 heads, 4,059 over 4,059 45.9
-  // in 16-query, 51.2 in 128-query tiles). Chunks of 33 to 63 tokens leave the
-  // 128-query tiles' 64-row units part masked, and few tiles lose to the 16-query
-  // blocks either way (48-token chunks, 32 heads, 1,499 over 1,499 48.9 / 39.2 /
-  // 53.2, 987 over 987 25.8 / 27.9 / 26.8).
-  // Over chunks of at most 32 tokens the 64-query tiles go wherever they are
-  // the faster by the same kind of model (two blocks a compute unit, ~0.87 us
-  // per pair of 32-row units, which hold two 16-token chunks; 300 queries over
-  // 1,300 positions in 16-token chunks: 80 us in one part of 16-query blocks,
-  // 65 in three, 23 so), but not for one or two chunks, which a 16-query block
-  // takes in one pair (2 heads, 16 queries over 16 positions in 16-token chunks 4.7
-  // us in 16-query blocks / 5.5 in 64-query tiles, 32 over 32 5.6 / 5.9, 48 over 48
-  // 7.3 / 6.3).
-  if (cache->prefill_split <= 1) {
-    const int64_t units32 = a.C == 16 ? (nc + 1) / 2 : static_cast<int64_t>(nc) * ((a.C + 31) / 32);
-    const double us64 = (tiles + 2 * cus - 1) / (2 * cus) * (5.0 + 0.87 * ((units32 + 1) / 2));
-    const int64_t tiles128 = (n_q + 127) / 128 * a.H;
-    // d = 64: rounds enough, or at least 2/7 of the path cached; units filled
-    const bool even = tiles128 >= 3 * cus || (4 * tiles128 >= 7 * cus && 7 * (L - n_q) >= 2 * L);
-    const bool filled = a.C >= 64 || a.C == 32 || a.C == 16;
-    if (tiles128 >= cus && (a.D == 128 || (even && filled))) a.tile_rows = 128;
-    else if (a.C <= 32 ? cache->prefill_split == 0 && nc > 2 && us64 < best_us
-             : a.D == 128 ? tiles > cus
-                          : tiles128 >= cus && (filled || 2 * tiles128 >= 3 * cus))
-      a.tile_rows = 64;
-    if (a.tile_rows > 0) split = 1;
-  }
+  const int64_t split = prefill_shape(cache, n_q, nc, L - n_q, L, &a.tile_rows);
   a.n_split = static_cast<int>(split);
   if (split > 1) {
+    const int64_t tiles = (n_q + 63) / 64 * static_cast<int64_t>(a.H);
     const size_t ws = static_cast<size_t>(tiles * split) * ca::prefill_part_bytes(a.D);
     if ((st = ensure_device(reinterpret_cast<char**>(&cache->d_pf_ws), &cache->d_pf_ws_cap, ws, s,
                             "prefill partials")) != CA_OK)

@@ -79,6 +79,8 @@ struct PrefillArgs {
   const int32_t* host_path;    // host [n_chunks] slots then [n_chunks + 1] starts, or null
   const int32_t* chunk_slot;   // device [n_chunks] (paths longer than the inline limit)
   const int32_t* chunk_start;  // device [n_chunks + 1]
+                               // windowed: only chunks that some query sees, [n_chunks]
+                               // starts, then [n_chunks] ends
   int n_chunks;
   int n_q;
   int L;         // positions of the path
@@ -95,6 +97,9 @@ struct PrefillArgs {
   size_t ws_bytes = 0;  // bytes of ws the launch may touch (below 4 GiB)
   int32_t* cnt = nullptr;
   int cnt_shift = 0;    // counter of tile t is cnt[t << cnt_shift] (tile_counter_shift)
+  // > 0: a windowed call, the query at position p sees the positions j <= p with
+  // j < sinks or j > p - window
+  int window = 0, sinks = 0;
 };
 constexpr size_t prefill_part_bytes(int D) { return (64 * static_cast<size_t>(D) + 128) * 4; }
 hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream);
@@ -208,34 +213,5 @@ struct Kv4PrefillArgs {
 };
 constexpr size_t kv4_prefill_part_bytes(int rows, int D) { return static_cast<size_t>(rows) * (D + 2) * 4; }
 hipError_t launch_kv4_prefill(const Kv4PrefillArgs& a, hipStream_t stream);
-
-// Prefill attention with a sliding window and sinks over an fp16 or a 4-bit
-// pool, and every prefill call over a 4-bit one (window_prefill.hip).
-struct WindowPrefillArgs {
-  int store;  // kStoreF16 or kStoreKv4
-  int H, D, C;
-  const void* q;
-  void* o;
-  const void* kpool;
-  const void* vpool;
-  int64_t ss, hs;  // pool strides of a slot and of a head (elements; bytes of a 4-bit pool)
-  // the chunks that some query sees, root -> leaf: slots, starts, ends, n_chunks
-  // each; on the host (up to kPrefillInlineChunks) or on the device
-  const int32_t* host_path;
-  const int32_t* path;
-  int n_chunks;
-  int n_q;
-  int L;  // positions of the sequence
-  int window, sinks;
-  float qscale;
-  int tile_rows;    // queries of a block's tile: 128 or 64
-  int n_split = 1;  // parts of a tile's keys, in blocks of their own
-  float* ws = nullptr;  // n_split > 1: window_prefill_part_bytes() per tile and part
-  size_t ws_bytes = 0;
-  int32_t* cnt = nullptr;  // n_split > 1: a zeroed counter per tile, left at zero
-  int cnt_shift = 0;
-};
-constexpr size_t window_prefill_part_bytes(int rows, int D) { return static_cast<size_t>(rows) * (D + 2) * 4; }
-hipError_t launch_window_prefill(const WindowPrefillArgs& a, hipStream_t stream);
 
 }  // namespace ca

@@ -3,6 +3,7 @@
 // prefill paragraph).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cstdint>
 #include <type_traits>
@@ -66,6 +67,7 @@ struct KpfParams {
   int cnt_shift;                // counter of tile t is cnt[t << cnt_shift] (tile_counter_shift)
   uint32_t ws_bytes;            // bytes of ws (below 4 GiB: 32-bit buffer offsets)
   int L;                        // positions of the path
+  int window, sinks;            // windowed calls, both at most L
 };
 
 // floats of one partial: unnormalised O of 64 query rows, their maxima and sums
@@ -90,15 +92,92 @@ struct KpfPath {
   int32_t slot[NI];
   int32_t start[NI + 1];
 };
+// A windowed call's holds only the chunks that some query sees, so that one may
+// end before the next begins.
+template <int NI>
+struct KpfWinPath {
+  int32_t slot[NI];
+  int32_t start[NI];
+  int32_t end[NI];
+};
+template <int NI, bool WIN>
+using KpfPathOf = std::conditional_t<WIN, KpfWinPath<(NI > 0 ? NI : 1)>, KpfPath<(NI > 0 ? NI : 1)>>;
+
+// Windowed calls (WIN): the query at position p sees the positions j <= p with
+// j < sinks or j > p - window. Of a tile's units, numbered along the path, those
+// in [0, ua) hold the sinks, those in [ub, ue) what its queries see besides; the
+// units between them are left out, and the loops run over the rest, numbered
+// without the gap. A unit that some query of a wavefront sees only in part is
+// masked at both ends, and may hold V elements that are not finite in rows that
+// a query does not see, which 0 * V would bring to it all the same: so its V
+// operands are looked at (one packed maximum per register), and where there is
+// such an element it counts as 0 and o becomes NaN for the queries that see it:
+// at once in the 16-query blocks; in the 32-query ones, whose loop has no
+// registers left for it, in a second pass over the tile.
+struct WinUnits {
+  int na = 0, nb = 0, ne = 0;  // chunks that start below the sinks; end at or below `lo`; start up to `last`
+  int a_start = 0, b_start = 0, e_start = 0;  // starts of chunks na - 1, nb, ne - 1
+  int ua = 0, ub = 0, n = 0;  // n: units of the tile
+  // chunks 64 i .. 64 i + 63, one a lane
+  __device__ __forceinline__ void count(int i, int start, int end, bool in, int sinks, int lo, int last) {
+    const int a = __popcll(__ballot(in && start < sinks)), b = __popcll(__ballot(in && end <= lo)),
+              e = __popcll(__ballot(in && start <= last));
+    if (a > 0) a_start = __builtin_amdgcn_readlane(start, a - 1);
+    if (nb == 64 * i && b < 64) b_start = __builtin_amdgcn_readlane(start, b);
+    if (e > 0) e_start = __builtin_amdgcn_readlane(start, e - 1);
+    na += a;
+    nb += b;
+    ne += e;
+  }
+  // units of TOK rows, upc of them a chunk of C
+  __device__ __forceinline__ void chunks_to_units(int tok, int upc, int C, int sinks, int lo, int last) {
+    const int ue = (ne - 1) * upc + min(last - e_start, C - 1) / tok + 1;
+    ua = na > 0 ? (na - 1) * upc + (min(sinks - a_start, C) + tok - 1) / tok : 0;
+    finish(ue, nb * upc + max(0, lo - b_start) / tok);
+  }
+  // units of G chunks
+  __device__ __forceinline__ void groups_to_units(int G) {
+    ua = (na + G - 1) / G;
+    finish((ne + G - 1) / G, nb / G);
+  }
+  __device__ __forceinline__ int real(int u) const { return u < ua ? u : u - ua + ub; }
+  // how many of the first k units of the path are the tile's
+  __device__ __forceinline__ int seen(int k) const { return k <= ua ? k : k <= ub ? ua : min(k - ub + ua, n); }
+
+ private:
+  __device__ __forceinline__ void finish(int ue, int from) {
+    ua = min(ua, ue);
+    ub = max(ua, from);
+    n = ua + max(0, ue - ub);
+  }
+};
+
+// the larger exponents and mantissas of 8 fp16 values, two at a time
+typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void abs_max(ushort2_t& m, half8 x) {
+  const u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t y = w[i] & 0x7fff7fffu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2_t, y));
+  }
+}
+__device__ __forceinline__ bool any_not_finite(ushort2_t m) {
+  return __any(max(static_cast<unsigned>(m[0]), static_cast<unsigned>(m[1])) >= 0x7c00u);
+}
+__device__ __forceinline__ bool not_finite(_Float16 x) {
+  return !(__builtin_fabsf(static_cast<float>(x)) < INFINITY);
+}
 
 // Work unit: TOK consecutive rows of one chunk (a chunk of up to c tokens
 // has ceil(c / TOK) units). NI > 0: the path comes in `path` (at most NI
-// chunks); NI == 0: in the device arrays cslot / cstart.
-template <int D, int NGRP, int WPG, int TOK, int NI>
+// chunks); NI == 0: in the device arrays cslot / cstart
+// (windowed calls: the chunks' ends behind their starts).
+template <int D, int NGRP, int WPG, int TOK, int NI, bool WIN>
 __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
                                                               const int32_t* __restrict__ cslot,
                                                               const int32_t* __restrict__ cstart,
-                                                              const KpfPath<(NI > 0 ? NI : 1)> path) {
+                                                              const KpfPathOf<NI, WIN> path) {
   constexpr int QT = 4 / WPG;       // 16-query tiles per wavefront
   constexpr int GT = 64 * WPG;      // threads per group
   constexpr int KS = D / 32;        // 16x16x32 steps over d
@@ -128,7 +207,8 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
     if (l < P.n_chunks) {
       lane_slot = path.slot[l];
       lane_start = path.start[l];
-      lane_end = path.start[l + 1];
+      if constexpr (WIN) lane_end = path.end[l];
+      else lane_end = path.start[l + 1];
     }
   }
   auto chunk_slot = [&](int j) -> int {
@@ -143,8 +223,9 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
   };
   auto chunk_end = [&](int j) -> int {
     if constexpr (kLane) return __builtin_amdgcn_readlane(lane_end, j);
+    else if constexpr (NI > 0 && WIN) return path.end[j];
     else if constexpr (NI > 0) return path.start[j + 1];
-    else return cstart[j + 1];
+    else return cstart[WIN ? P.n_chunks + j : j + 1];
   };
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -181,7 +262,7 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
     for (int s = 0; s < KS; ++s)
       qf[t][s] = *reinterpret_cast<const half8*>(P.q + (static_cast<size_t>(qr) * H + h) * D + 32 * s + 8 * g);
   }
-  const int L = chunk_end(P.n_chunks - 1);
+  const int L = WIN ? P.L : chunk_end(P.n_chunks - 1);
   const int pos_last = L - n_q + min(q0 + 63, n_q - 1);        // last position of the tile
   const int pos_first = L - n_q + q0;                          // first position of the tile
   const size_t slot_stride = static_cast<size_t>(P.ss);
@@ -210,7 +291,17 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
   // (starts ascend); 64 starts per load, one per lane.
   const int nc = P.n_chunks;
   int n_ch = 0;
-  if constexpr (kLane) {
+  WinUnits wu;
+  if constexpr (WIN) {
+    const int lo = max(0, pos_first - P.window + 1);
+    for (int i = 0; 64 * i < nc; ++i) {
+      const int j = 64 * i + lane;
+      const bool in = j < nc;
+      if constexpr (kLane) wu.count(i, lane_start, lane_end, in, P.sinks, lo, pos_last);
+      else wu.count(i, chunk_start(in ? j : 0), chunk_end(in ? j : 0), in, P.sinks, lo, pos_last);
+    }
+    wu.chunks_to_units(TOK, upc, P.C, P.sinks, lo, pos_last);
+  } else if constexpr (kLane) {
     n_ch = __popcll(__ballot(lane_start <= pos_last));
   } else {
     for (int b = 0; b < nc; b += 64) {
@@ -220,13 +311,14 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
       if (m != ~0ull) break;
     }
   }
-  const int n_units = n_ch * upc;
+  const int n_units = WIN ? wu.n : n_ch * upc;
   // this block's part of the tile's units
   const int u_lo = static_cast<int>(static_cast<int64_t>(n_units) * part / S);
   const int u_hi = static_cast<int>(static_cast<int64_t>(n_units) * (part + 1) / S);
   // unit u is rows r0 .. r0 + TOK - 1 of chunk j (no division when every
   // chunk is one unit; uniform)
   auto unit_pos = [&](int u, int& j, int& r0) {
+    if constexpr (WIN) u = wu.real(u);
     if (upc == 1) {
       j = u;
       r0 = 0;
@@ -323,16 +415,21 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
     // lane holds S^T[token 16jt + 4g + i][row l16 of tile t] (unscaled).
     // Units that are whole and end before the tile's first position need no
     // mask (uniform test).
-    if (len < TOK || c0 + TOK - 1 > pos_first) {
+    const bool edge = WIN && c0 <= pos_last - P.window && c0 + TOK > P.sinks;  // a lower end inside the unit
+    const bool masked = len < TOK || c0 + TOK - 1 > pos_first || edge;
+    auto seen = [&](int t, int tk) {
+      bool y = tk < len && c0 + tk <= pos[t];
+      if constexpr (WIN) y = y && (c0 + tk < P.sinks || c0 + tk > pos[t] - P.window);
+      return y;
+    };
+    if (masked) {
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
         for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tk = 16 * jt + 4 * g + i;
-            if (!(tk < len && c0 + tk <= pos[t])) sacc[t][jt][i] = -INFINITY;
-          }
+          for (int i = 0; i < 4; ++i)
+            if (!seen(t, 16 * jt + 4 * g + i)) sacc[t][jt][i] = -INFINITY;
     }
     half8 pb[QT][PV];
     bool moved = false;
@@ -381,17 +478,66 @@ __global__ __launch_bounds__(64 * WPG * NGRP) void kpf_kernel(KpfParams P,
         nacc[t] *= alpha[t];
       }
     }
+    auto read_v = [&](int dt, int p2) {
+      const _Float16* vp = v_lds + (32 * p2 + 4 * g + (l16 >> 2)) * VST + 16 * dt + 4 * (l16 & 3);
+      const half4 v0 = lds_read_tr16(vp);             // tokens 32p + 4g + j
+      const half4 v1 = lds_read_tr16(vp + 16 * VST);  // tokens 32p + 16 + 4g + j
+      return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    bool bad = false;  // a V element that is not finite, in a masked unit
+    if constexpr (WIN) {
+      if (masked) {
+        ushort2_t m = {0, 0};
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int p2 = 0; p2 < PV; ++p2) {
-        const _Float16* vp = v_lds + (32 * p2 + 4 * g + (l16 >> 2)) * VST + 16 * dt + 4 * (l16 & 3);
-        const half4 v0 = lds_read_tr16(vp);             // tokens 32p + 4g + j
-        const half4 v1 = lds_read_tr16(vp + 16 * VST);  // tokens 32p + 16 + 4g + j
-        const half8 va = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+          for (int p2 = 0; p2 < PV; ++p2) abs_max(m, read_v(dt, p2));
+        bad = any_not_finite(m);
+      }
+    }
+    if (WIN && bad) {
+#pragma unroll 1
+      for (int dt0 = 0; dt0 < DT; ++dt0) {
+        half8 x[PV], y[PV];
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
-          acc[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[t][p2], acc[t][dt], 0, 0, 0);
+        for (int p2 = 0; p2 < PV; ++p2) {
+          x[p2] = read_v(dt0, p2);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool b = not_finite(x[p2][e]);
+            y[p2][e] = static_cast<_Float16>(b ? 1.f : 0.f);
+            x[p2][e] = b ? static_cast<_Float16>(0.f) : x[p2][e];
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          floatx4 z = {0.f, 0.f, 0.f, 0.f}, o = z;
+#pragma unroll
+          for (int p2 = 0; p2 < PV; ++p2) {
+            half8 s;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              s[e] = static_cast<_Float16>(seen(t, 32 * p2 + 16 * (e >> 2) + 4 * g + (e & 3)) ? 1.f : 0.f);
+            z = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[p2], s, z, 0, 0, 0);
+            o = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[p2], pb[t][p2], o, 0, 0, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = z[i] > 0.f ? __builtin_nanf("") : o[i];
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)  // dt0 is not a constant: registers
+            if (dt == dt0) acc[t][dt] += o;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+        for (int p2 = 0; p2 < PV; ++p2) {
+          const half8 va = read_v(dt, p2);
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            acc[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(va, pb[t][p2], acc[t][dt], 0, 0, 0);
+        }
       }
     }
     // n += the sum of P over the unit's tokens, from the same fp16 P as O:
@@ -614,10 +760,10 @@ typedef float float2_t __attribute__((ext_vector_type(2)));
 // rows fall into (a unit per 16-token chunk left three quarters of every unit
 // masked: 1,000 queries over 1,500 positions in 16-token chunks 128 -> 35.5 us,
 // in 32-token chunks 67 -> 32; 2,000 over 6,000 in 16-token chunks 827 -> 207).
-template <int D, int QW, int KG, int TOK, int CC, int NI>
+template <int D, int QW, int KG, int TOK, int CC, int NI, bool WIN>
 __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const int32_t* __restrict__ cslot,
                                                               const int32_t* __restrict__ cstart,
-                                                              const KpfPath<(NI > 0 ? NI : 1)> path) {
+                                                              const KpfPathOf<NI, WIN> path) {
   constexpr int QR = 32 * QW;       // query rows of a tile
   constexpr int KS = D / 16;        // 32x32x16 steps over d
   constexpr int DT = D / 32;        // 32-wide d tiles of O^T
@@ -638,9 +784,14 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     if constexpr (NI > 0) return path.slot[j];
     else return cslot[j];
   };
-  auto chunk_start = [&](int j) -> int {  // j up to n_chunks
+  auto chunk_start = [&](int j) -> int {
     if constexpr (NI > 0) return path.start[j];
     else return cstart[j];
+  };
+  auto chunk_end = [&](int j) -> int {
+    if constexpr (NI > 0 && WIN) return path.end[j];
+    else if constexpr (NI > 0) return path.start[j + 1];
+    else return cstart[WIN ? P.n_chunks + j : j + 1];
   };
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -695,7 +846,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     const bool in = j < nc;
     w_off = static_cast<int64_t>(chunk_slot(in ? j : 0)) * P.ss;
     w_start = in ? chunk_start(j) : kNoPos;
-    w_end = in ? chunk_start(j + 1) : kNoPos;
+    w_end = in ? chunk_end(j) : kNoPos;
     // wait here, not where the loop reads them (that wait would also cover
     // the rows requested for later steps)
     asm volatile("" : "+v"(w_start), "+v"(w_end), "+v"(w_off));
@@ -704,16 +855,23 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
   // chunks the tile needs, and those the wavefront's queries can see: a
   // prefix of the path each (starts ascend)
   int n_ch = 0, n_vis = 0;
+  WinUnits wu;
+  const int lo = WIN ? max(0, L - n_q + q0 - P.window + 1) : 0;
   for (int wi = 0;;) {
     n_ch += __popcll(__ballot(w_start <= pos_last));
     n_vis += __popcll(__ballot(w_start <= pos_first + 31));
+    if constexpr (WIN) wu.count(wi, w_start, w_end, 64 * wi + lane < nc, P.sinks, lo, pos_last);
     if (n_ch < 64 * ++wi || 64 * wi >= nc) break;
     load_window(wi);
   }
-  const int n_units = CC > 0 ? (n_ch + G - 1) / G : n_ch * upc;  // at least one
+  if constexpr (WIN && CC > 0) wu.groups_to_units(G);
+  else if constexpr (WIN) wu.chunks_to_units(TOK, upc, P.C, P.sinks, lo, pos_last);
+  const int n_units = WIN ? wu.n : CC > 0 ? (n_ch + G - 1) / G : n_ch * upc;  // at least one
   const int steps = (n_units + KG - 1) / KG;
   // steps of this group whose unit the wavefront sees something of (may be <= 0)
-  const int n_see = ((CC > 0 ? (n_vis + G - 1) / G : n_vis * upc) - grp + KG - 1) / KG;
+  const int vis_units = CC > 0 ? (n_vis + G - 1) / G : n_vis * upc;
+  const int n_see = ((WIN ? wu.seen(vis_units) : vis_units) - grp + KG - 1) / KG;
+  const uint32_t upc_inv = WIN && upc > 1 ? 0xffffffffu / static_cast<unsigned>(upc) + 1u : 0u;
 
   struct Unit {
     int64_t off[G];          // first row of each chunk in a head's pool (elements)
@@ -724,6 +882,16 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
   // descriptors of the group's units in order; past the end the last one again
   int fu = min(grp, n_units - 1);
   int fj = CC > 0 ? fu * G : upc == 1 ? fu : fu / upc, fr = CC > 0 || upc == 1 ? 0 : fu - fj * upc;
+  auto locate = [&]() {  // windowed calls: chunk and piece of unit fu
+    const int k = wu.real(fu);
+    if constexpr (CC > 0) {
+      fj = k * G;
+    } else {
+      fj = upc == 1 ? k : static_cast<int>(__umulhi(static_cast<unsigned>(k), upc_inv));
+      fr = k - fj * upc;
+    }
+  };
+  if constexpr (WIN) locate();
   auto fetch = [&]() {  // after turn_window(); no branches
     Unit d;
     const int l0 = fj & 63;
@@ -740,13 +908,15 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     bool whole = true;
 #pragma unroll
     for (int q = 1; q < G; ++q) {
-      whole &= d.clen[q] == 0 || d.clen[q - 1] == CC;
+      whole &= d.clen[q] == 0 || (d.clen[q - 1] == CC && (!WIN || d.cpos[q] == d.cpos[q - 1] + CC));
       d.len += d.clen[q];
     }
     d.len = whole ? d.len : -1;
     const bool more = fu + KG < n_units;
     fu += more ? KG : 0;
-    if constexpr (CC > 0) {
+    if constexpr (WIN) {
+      locate();
+    } else if constexpr (CC > 0) {
       fj += more ? KG * G : 0;
     } else {
       fr += more ? KG : 0;
@@ -858,32 +1028,55 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
       for (int r = 0; r < 16; ++r) c[r & 3] = fmaxf(c[r & 3], sa[jt][r]);
     lmax = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
   };
-  // -inf where the unit's tokens are past its rows or after the query; done
-  // only for units that have such tokens (uniform), with their maximum again
-  auto mask = [&](floatx16 (&sa)[JT], const Unit& d) {
-    if (d.len >= TOK && d.pos + TOK - 1 <= pos_first) return;
+  // -inf where the unit's tokens are past its rows, after the query or out of
+  // its window; done only for units that have such tokens (uniform), with their
+  // maximum again. Windowed calls: whether the unit has such tokens; with BITS
+  // and in hid, a bit for each of the lane's tokens that its query does not see,
+  // the first token's the highest
+  bool part = false;
+  uint32_t hid = 0;
+  auto mask = [&](floatx16 (&sa)[JT], const Unit& d, auto bits) {
+    constexpr bool BITS = decltype(bits)::value;
+    const bool edge = WIN && d.pos <= pos_first + 31 - P.window && d.pos + TOK > P.sinks;
+    part = !(d.len >= TOK && d.pos + TOK - 1 <= pos_first && !edge);
+    if constexpr (BITS) hid = 0;
+    if (!part) return;
+    // min with +inf for a visible token, -inf for another: three vector ops
+    // per element and no lane masks (32 of them spill the scalar registers)
+    auto masked = [&](float y, int x) {  // x < 0: not seen
+      if constexpr (BITS) hid = __builtin_amdgcn_alignbit(hid, static_cast<uint32_t>(x), 31);
+      return fminf(y, __int_as_float((x & INT32_MIN) | 0x7f800000));
+    };
+    // the query's window starts at position pos - P.window + 1 (at most L, so
+    // the differences below do not wrap)
+    const int wlo = WIN ? max(pos - P.window, -1) + 1 : 0;
     if (CC > 0 && d.len < 0) {  // a short chunk inside the unit: chunk by chunk
 #pragma unroll
       for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           constexpr int C1 = CC > 0 ? CC : 1;
-          const int t = 32 * jt + 8 * (r >> 2), q = t / C1 % G;
-          const int x = min(d.clen[q] - 1, pos - d.cpos[q]) - 4 * hl - (t % C1 + (r & 3));
-          sa[jt][r] = fminf(sa[jt][r], __int_as_float((x & INT32_MIN) | 0x7f800000));
+          const int t = 32 * jt + 8 * (r >> 2), q = t / C1 % G, k = t % C1 + (r & 3);
+          int x = min(d.clen[q] - 1, pos - d.cpos[q]) - 4 * hl - k;
+          if constexpr (WIN) {
+            const int at = d.cpos[q] + 4 * hl + k;
+            x |= (P.sinks - 1 - at) & (at - wlo);
+          }
+          sa[jt][r] = masked(sa[jt][r], x);
         }
       rowmax(sa);
       return;
     }
-    // min with +inf for a visible token, -inf for another: three vector ops
-    // per element and no lane masks (32 of them spill the scalar registers)
     const int last = min(d.len - 1, pos - d.pos) - 4 * hl;  // last visible token of the unit
+    const int sk = P.sinks - 1 - d.pos - 4 * hl, wl = wlo - d.pos - 4 * hl;
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int x = last - (32 * jt + 8 * (r >> 2) + (r & 3));
-        sa[jt][r] = fminf(sa[jt][r], __int_as_float((x & INT32_MIN) | 0x7f800000));
+        const int t = 32 * jt + 8 * (r >> 2) + (r & 3);
+        int x = last - t;
+        if constexpr (WIN) x |= (sk - t) & (t - wl);
+        sa[jt][r] = masked(sa[jt][r], x);
       }
     rowmax(sa);
   };
@@ -972,11 +1165,20 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
   if (n_see > 0) {
     scores(sA, 0);
     rowmax(sA);
-    mask(sA, d0);
+    mask(sA, d0, std::false_type{});
     refmax();
   }
   // B0, the tile of unit i, is a constant, so that every LDS address is a
   // register fixed for the whole call plus an immediate offset
+  // (windowed calls) a unit that some query sees in part: whether its V has an
+  // element that is not finite
+  bool bad = false;
+  auto look_at_v = [&](int b) {
+    ushort2_t m = {0, 0};
+#pragma unroll
+    for (int k = 0; k < NO; ++k) abs_max(m, read_v(b, k / DT, k % DT));
+    bad |= any_not_finite(m);
+  };
   auto step = [&](auto b0c, int i, floatx16 (&cur)[JT], floatx16 (&nxt)[JT]) {
     constexpr int b0 = decltype(b0c)::value, b1 = 1 - b0;
     landed();  // (step 0: K(0) has been read)
@@ -985,6 +1187,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     issue_v(d1, b1);
     if (i < n_see) {
       scores_probs(cur, nxt, b1, b0);
+      if (WIN && part) look_at_v(b0);
       // O^T += V^T P^T, and the next unit's row maxima
       float c[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -997,7 +1200,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
         fence();
       }
       lmax = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
-      mask(nxt, d1);
+      mask(nxt, d1, std::false_type{});
       refmax();
     }
     turn_window();
@@ -1008,6 +1211,57 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     if (i + 1 < steps) step(std::integral_constant<int, 1>{}, i + 1, sB, sA);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load writes LDS after this
+  if constexpr (WIN) {
+    // Such an element in some wavefront's unit (never in ordinary data): the
+    // tile over again, unit after unit, with those elements as 0, and NaN for
+    // the queries that see one.
+    if (__syncthreads_or(bad)) {
+      m_run = kNegBig;
+      n_run = n2 = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+      fu = min(grp, n_units - 1);
+      locate();
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i) {
+        const Unit d = next();
+        __syncthreads();  // the tiles have been read
+        issue_k(d, 0);
+        issue_v(d, 0);
+        landed();
+        if (i >= n_see) continue;
+        scores(sA, 0);
+        rowmax(sA);
+        mask(sA, d, std::true_type{});
+        refmax();
+#pragma unroll
+        for (int e = 0; e < 16 * JT; e += 2) prob2(sA, e);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          floatx16 z;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) z[k] = 0.f;
+#pragma unroll
+          for (int p = 0; p < 2 * JT; ++p) {
+            half8 x = read_v(0, p, dt), y, see;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool f = not_finite(x[e]);
+              y[e] = static_cast<_Float16>(f ? 1.f : 0.f);
+              x[e] = f ? static_cast<_Float16>(0.f) : x[e];
+              see[e] = static_cast<_Float16>(hid >> (16 * JT - 1 - (8 * p + e)) & 1 ? 0.f : 1.f);
+            }
+            z = __builtin_amdgcn_mfma_f32_32x32x16_f16(y, see, z, 0, 0, 0);
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, pb[p], acc[dt], 0, 0, 0);
+          }
+#pragma unroll
+          for (int k = 0; k < 16; ++k) acc[dt][k] = z[k] > 0.f ? __builtin_nanf("") : acc[dt][k];
+        }
+      }
+    }
+  }
   // the row's sum over both halves of the wavefront
   n_run += n2;
   float n_row = n_run + __shfl_xor(n_run, 32);
@@ -1064,32 +1318,59 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     }
 }
 
-template <int D, int QW, int KG, int TOK, int CC>
+// the path as the kernel takes it
+template <int NI, bool WIN>
+KpfPathOf<NI, WIN> path_of(const PrefillArgs& a) {
+  KpfPathOf<NI, WIN> path{};
+  if constexpr (NI > 0) {
+    for (int j = 0; j < a.n_chunks; ++j) path.slot[j] = a.host_path[j];
+    for (int j = 0; j < a.n_chunks + (WIN ? 0 : 1); ++j) path.start[j] = a.host_path[a.n_chunks + j];
+    if constexpr (WIN)
+      for (int j = 0; j < a.n_chunks; ++j) path.end[j] = a.host_path[2 * a.n_chunks + j];
+  }
+  return path;
+}
+constexpr int kLaneChunks = 64;  // paths up to this long: kernels of their own
+
+template <int D, int QW, int KG, int TOK, int CC, bool WIN>
 void launch_wide_cc(const KpfParams& P, const PrefillArgs& a, hipStream_t stream) {
-  constexpr int kLaneChunks = 64;
   const int blocks = (a.n_q + 32 * QW - 1) / (32 * QW) * a.H;
   const dim3 grid(8 * ((blocks + 7) / 8)), block(64 * QW * KG);  // a multiple of the XCD count
-  if (a.host_path && a.n_chunks <= kLaneChunks) {
-    KpfPath<kLaneChunks> path;
-    for (int j = 0; j < a.n_chunks; ++j) path.slot[j] = a.host_path[j];
-    for (int j = 0; j <= a.n_chunks; ++j) path.start[j] = a.host_path[a.n_chunks + j];
-    kpw_kernel<D, QW, KG, TOK, CC, kLaneChunks><<<grid, block, 0, stream>>>(P, nullptr, nullptr, path);
-  } else if (a.host_path) {
-    KpfPath<kPrefillInlineChunks> path;
-    for (int j = 0; j < a.n_chunks; ++j) path.slot[j] = a.host_path[j];
-    for (int j = 0; j <= a.n_chunks; ++j) path.start[j] = a.host_path[a.n_chunks + j];
-    kpw_kernel<D, QW, KG, TOK, CC, kPrefillInlineChunks><<<grid, block, 0, stream>>>(P, nullptr, nullptr, path);
-  } else {
-    const KpfPath<1> none{};
-    kpw_kernel<D, QW, KG, TOK, CC, 0><<<grid, block, 0, stream>>>(P, a.chunk_slot, a.chunk_start, none);
-  }
+  auto call = [&](auto ni) {
+    constexpr int NI = decltype(ni)::value;
+    kpw_kernel<D, QW, KG, TOK, CC, NI, WIN><<<grid, block, 0, stream>>>(P, a.chunk_slot, a.chunk_start,
+                                                                       path_of<NI, WIN>(a));
+  };
+  if (!a.host_path) call(std::integral_constant<int, 0>{});
+  else if (!WIN && a.n_chunks <= kLaneChunks) call(std::integral_constant<int, WIN ? 0 : kLaneChunks>{});
+  else call(std::integral_constant<int, kPrefillInlineChunks>{});
 }
 
-template <int D, int QW, int KG, int TOK>
+template <int D, int QW, int KG, int TOK, bool WIN>
 void launch_wide(const KpfParams& P, const PrefillArgs& a, hipStream_t stream) {
-  if (a.C == 16) launch_wide_cc<D, QW, KG, TOK, 16>(P, a, stream);
-  else if (TOK == 64 && a.C == 32) launch_wide_cc<D, QW, KG, TOK, TOK == 64 ? 32 : 0>(P, a, stream);
-  else launch_wide_cc<D, QW, KG, TOK, 0>(P, a, stream);
+  if (a.C == 16) launch_wide_cc<D, QW, KG, TOK, 16, WIN>(P, a, stream);
+  else if (TOK == 64 && a.C == 32) launch_wide_cc<D, QW, KG, TOK, TOK == 64 ? 32 : 0, WIN>(P, a, stream);
+  else launch_wide_cc<D, QW, KG, TOK, 0, WIN>(P, a, stream);
+}
+
+template <int D, bool WIN>
+void launch_d(const KpfParams& P, const PrefillArgs& a, hipStream_t stream) {
+  if (a.tile_rows == 128) return launch_wide<D, 4, 1, 64, WIN>(P, a, stream);
+  if (a.tile_rows == 64) return launch_wide<D, 2, 2, 32, WIN>(P, a, stream);
+  // two groups of four wavefronts (16 queries each), 64-row units, two LDS
+  // tiles per group
+  constexpr int kGroups = 2, kWaves = 4, kTok = 64;
+  const int blocks = ((a.n_q + 63) / 64) * a.H * a.n_split;
+  const dim3 grid(8 * ((blocks + 7) / 8)), block(64 * kWaves * kGroups);  // a multiple of the XCD count
+  auto call = [&](auto ni) {
+    constexpr int NI = decltype(ni)::value;
+    kpf_kernel<D, kGroups, kWaves, kTok, NI, WIN><<<grid, block, 0, stream>>>(P, a.chunk_slot, a.chunk_start,
+                                                                             path_of<NI, WIN>(a));
+  };
+  if (!a.host_path) call(std::integral_constant<int, 0>{});
+  // these keep their chunk table in the lanes of a register
+  else if (a.n_chunks <= kLaneChunks) call(std::integral_constant<int, kLaneChunks>{});
+  else call(std::integral_constant<int, kPrefillInlineChunks>{});
 }
 
 }  // namespace
@@ -1099,64 +1380,15 @@ hipError_t launch_prefill(const PrefillArgs& a, hipStream_t stream) {
   KpfParams P{static_cast<const _Float16*>(a.q), static_cast<_Float16*>(a.o),
               static_cast<const _Float16*>(a.kpool), static_cast<const _Float16*>(a.vpool), a.ss,
               a.hs, a.n_chunks, a.n_q, a.H, a.C, a.qscale, a.n_split, a.ws, a.cnt, a.cnt_shift,
-              static_cast<uint32_t>(a.ws_bytes), a.L};
+              static_cast<uint32_t>(a.ws_bytes), a.L, std::min(a.window, a.L), std::min(a.sinks, a.L)};
   if (a.n_split < 1 || (a.n_split > 1 && (!a.ws || !a.cnt || a.ws_bytes > 0xFFFFFFF0ull)))
     return hipErrorInvalidValue;
   if (a.host_path ? a.n_chunks > kPrefillInlineChunks : !a.chunk_slot) return hipErrorInvalidValue;
-  if (a.tile_rows == 128 && a.n_split == 1) {
-    if (a.D == 128) launch_wide<128, 4, 1, 64>(P, a, stream);
-    else if (a.D == 64) launch_wide<64, 4, 1, 64>(P, a, stream);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
-  }
-  if (a.tile_rows == 64 && a.n_split == 1) {
-    if (a.D == 128) launch_wide<128, 2, 2, 32>(P, a, stream);
-    else if (a.D == 64) launch_wide<64, 2, 2, 32>(P, a, stream);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
-  }
-  // two groups of four wavefronts (16 queries each), 64-row units, two LDS
-  // tiles per group
-  constexpr int kGroups = 2, kWaves = 4, kTok = 64;
-  // paths up to this long keep their chunk table in the lanes of a register
-  constexpr int kLaneChunks = 64;
-  const int blocks = ((a.n_q + 63) / 64) * a.H * a.n_split;
-  const dim3 grid(8 * ((blocks + 7) / 8));  // a multiple of the XCD count
-  const dim3 block(64 * kWaves * kGroups);
-  if (a.host_path && a.n_chunks <= kLaneChunks) {
-    KpfPath<kLaneChunks> path;
-    for (int j = 0; j < a.n_chunks; ++j) path.slot[j] = a.host_path[j];
-    for (int j = 0; j <= a.n_chunks; ++j) path.start[j] = a.host_path[a.n_chunks + j];
-    if (a.D == 128)
-      kpf_kernel<128, kGroups, kWaves, kTok, kLaneChunks><<<grid, block, 0, stream>>>(
-          P, nullptr, nullptr, path);
-    else if (a.D == 64)
-      kpf_kernel<64, kGroups, kWaves, kTok, kLaneChunks><<<grid, block, 0, stream>>>(
-          P, nullptr, nullptr, path);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
-  }
-  if (a.host_path && a.n_chunks <= kPrefillInlineChunks) {
-    KpfPath<kPrefillInlineChunks> path;
-    for (int j = 0; j < a.n_chunks; ++j) path.slot[j] = a.host_path[j];
-    for (int j = 0; j <= a.n_chunks; ++j) path.start[j] = a.host_path[a.n_chunks + j];
-    if (a.D == 128)
-      kpf_kernel<128, kGroups, kWaves, kTok, kPrefillInlineChunks><<<grid, block, 0, stream>>>(
-          P, nullptr, nullptr, path);
-    else if (a.D == 64)
-      kpf_kernel<64, kGroups, kWaves, kTok, kPrefillInlineChunks><<<grid, block, 0, stream>>>(
-          P, nullptr, nullptr, path);
-    else return hipErrorInvalidValue;
-    return hipGetLastError();
-  }
-  if (!a.chunk_slot) return hipErrorInvalidValue;
-  const KpfPath<1> none{};
-  if (a.D == 128)
-    kpf_kernel<128, kGroups, kWaves, kTok, 0><<<grid, block, 0, stream>>>(P, a.chunk_slot,
-                                                                         a.chunk_start, none);
-  else if (a.D == 64)
-    kpf_kernel<64, kGroups, kWaves, kTok, 0><<<grid, block, 0, stream>>>(P, a.chunk_slot,
-                                                                        a.chunk_start, none);
+  if (a.tile_rows != 0 && (a.n_split > 1 || (a.tile_rows != 64 && a.tile_rows != 128))) return hipErrorInvalidValue;
+  if (a.D == 128 && a.window > 0) launch_d<128, true>(P, a, stream);
+  else if (a.D == 128) launch_d<128, false>(P, a, stream);
+  else if (a.D == 64 && a.window > 0) launch_d<64, true>(P, a, stream);
+  else if (a.D == 64) launch_d<64, false>(P, a, stream);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

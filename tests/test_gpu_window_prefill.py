@@ -9,7 +9,7 @@ import torch
 from paper_2402_15220_amd.binding import ChunkAttnError
 from paper_2402_15220_amd.cache import Cache
 from parity_util import to_dev
-from window_util import WPair, assert_near, kv4_prefill_slack, random_tree, rows_of
+from window_util import WPair, assert_near, random_tree, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -31,11 +31,8 @@ def test_random_trees(kv, case):
         for n_q in sorted({1, min(L, 5), min(L, 63), min(L, 65), min(L, 130), L}):
             q = rng.standard_normal((n_q, H, d)).astype(np.float16)
             for window, sinks in ((1, 0), (1, 2), (40, 3), (64, 0), (129, 20), (L, 1), (10 ** 12, 0)):
-                scale = 1 / np.sqrt(d) if n_q % 2 else 0.2
                 o, ref = p.prefill(sid, q, window, sinks, scale=0.0 if n_q % 2 else 0.2)
-                slack = kv4_prefill_slack(p.tree, sid, q, window, sinks, scale) if kv == "kv4" else 0.0
-                assert_near(o, ref, np.float16, f"{kv} c={c} d={d} L={L} n_q={n_q} window={window} sinks={sinks}",
-                            slack)
+                assert_near(o, ref, np.float16, f"{kv} c={c} d={d} L={L} n_q={n_q} window={window} sinks={sinks}")
             if kv == "kv4":
                 o, ref = p.prefill(sid, q)
                 assert_near(o, ref, np.float16, f"{kv} c={c} d={d} L={L} n_q={n_q}")
