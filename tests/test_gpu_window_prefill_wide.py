@@ -47,7 +47,9 @@ def run(kv, H, d, c, L, n_q, window, sinks, bad, seed):
         ref = head_ref(q[:, h], kk[:, h], vv[:, h], L, window, sinks)
         ok = np.isfinite(ref)
         assert np.array_equal(np.isfinite(o[:, h]), ok), (h, np.argwhere(np.isfinite(o[:, h]) != ok)[:5])
-        assert ok.any()
+        assert ok.any() or (kv == "kv4" and sinks)  # there a row among the sinks is NaN throughout
+        if not ok.any():
+            continue
         assert_near(o[:, h][ok][None], ref[ok][None], np.float16, f"head {h}")
     p.cache.close()
 
@@ -74,6 +76,6 @@ def test_not_finite(shape, bad):
 
 
 @pytest.mark.parametrize("shape", [SHAPES[i] for i in (0, 1, 3, 5, 8, 10)])
-@pytest.mark.parametrize("bad", [None, np.nan])
-def test_4_bits(shape, bad):
-    run("kv4", *shape, 333, 5, bad, 43)
+@pytest.mark.parametrize("bad,sinks", [(None, 5), (np.nan, 5), (np.nan, 0)])
+def test_4_bits(shape, bad, sinks):
+    run("kv4", *shape, 333, sinks, bad, 43)
