@@ -273,7 +273,11 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
  * and lengths are read on the device, so appends that only fill chunks need
  * no upload. ca_set_tuning does not apply. While `stream` is being captured
  * into a graph nothing is allocated or uploaded: INVALID is returned unless
- * ca_prepare_window and one call (for the counters) came before.
+ * ca_prepare_window and one call (for the counters and the rows' order) came
+ * before. A captured call follows appends that only fill chunks; it is right
+ * until the next other change of the tree, and a replay after that is safe but
+ * sees the sequences as they were captured (what the call reads and writes of
+ * the library's memory is kept for it until ca_destroy; ws is the caller's).
  * Errors: INVALID (table-only cache, null or misaligned q/o, bad scale,
  * window or sinks, bad seq_ids, context not current under capture),
  * WORKSPACE, DEVICE. No live sequence is a no-op. */
@@ -337,10 +341,12 @@ ca_status ca_prefill_attention(ca_cache* cache, int64_t seq_id, const void* q, v
  * each query). Chunks that no query of the call sees are not read, and values
  * that a query does not see, NaN and infinite ones among them, do not reach
  * its o; where it sees a V element that is not finite its o is not finite
- * there. fp16 and 4-bit caches; a 4-bit cache's values are taken as fp16,
- * low + scale * code with one rounding. A call being captured is refused
- * (INVALID) where more than 255 chunks are seen or the library's partials
- * would have to grow. Errors as ca_prefill_attention. */
+ * there. fp16 and 4-bit caches; a 4-bit cache's values are taken as they are,
+ * low + scale * code, and softmax scales from 2^-29 to 2^23 (others are
+ * INVALID, for ca_prefill_attention over such a cache too). A call being captured is
+ * refused (INVALID) where more than 255 chunks are seen or the library's
+ * partials would have to grow; replays compute the tokens of the captured
+ * call. Errors as ca_prefill_attention. */
 ca_status ca_prefill_window(ca_cache* cache, int64_t seq_id, const void* q, void* o, int64_t n_q,
                             int64_t window, int64_t sinks, float scale, void* stream);
 

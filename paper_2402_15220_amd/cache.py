@@ -77,6 +77,8 @@ class Cache:
         else:
             raise ValueError(f"unknown layout {layout!r}")
         self._ws = None
+        self._ws_in_graph = False
+        self._kept = []
         self._dev_index = None if table_only else self.k_pool.device.index
 
     # -- helpers -----------------------------------------------------------
@@ -167,6 +169,9 @@ class Cache:
         else:
             need = B.ca_workspace_size(self.h)
         if self._ws is None or self._ws.numel() < need:
+            if self._ws_in_graph:  # a captured call writes there
+                self._kept.append(self._ws)
+                self._ws_in_graph = False
             self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.k_pool.device)
         return self._ws, need
 
@@ -184,6 +189,8 @@ class Cache:
             out = torch.empty_like(q)
         self._check_rows(out, Bn, "out")
         ws, need = self.workspace(window, sinks)
+        if torch.cuda.is_current_stream_capturing():
+            self._ws_in_graph = True
         if window is not None:
             B.ca_attention_window(self.h, q.data_ptr(), out.data_ptr(), seq_ids, window, sinks, scale,
                                   ws.data_ptr(), ws.numel(), self.stream())

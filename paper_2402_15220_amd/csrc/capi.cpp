@@ -160,6 +160,7 @@ struct PlanSlot {
   ca::Plan plan;
   bool valid = false;     // matches the tree
   bool uploaded = false;  // the device copy matches the plan
+  bool in_graph = false;  // a captured call reads the device copy
   uint64_t used = 0;      // when it was last asked for
   char* d = nullptr;
   size_t cap = 0;
@@ -217,6 +218,19 @@ struct ca_cache {
   PlanSlot plans[2];
   uint64_t plan_clock = 0;
 
+  // Device buffers that a captured call over a plan, or a captured windowed
+  // prefill, uses are neither given back nor written anew while the cache lives:
+  // a graph replayed late finds what it was captured with.
+  bool cnt_in_graph = false, rowmap_in_graph = false, pf_in_graph = false;
+  std::vector<void*> kept;
+  template <class T>
+  void leave_to_graph(T** p, size_t* cap, bool in_graph) {
+    if (!in_graph || !*p) return;
+    kept.push_back(*p);
+    *p = nullptr;
+    *cap = 0;
+  }
+
   // host export buffers
   ca::Tables exported;
 
@@ -234,6 +248,7 @@ struct ca_cache {
     if (d_pf_cnt) (void)hipFree(d_pf_cnt);
     for (PlanSlot& p : plans)
       if (p.d) (void)hipFree(p.d);
+    for (void* p : kept) (void)hipFree(p);
   }
 
   bool kv4() const { return cfg.dtype == CA_FP16_KV4; }
@@ -414,6 +429,8 @@ struct ca_cache {
     p->o_chunks = align_up(bi, 16);
     p->o_rows = p->o_chunks + align_up(bc, 16);
     const size_t total = p->o_rows + br;
+    leave_to_graph(&p->d, &p->cap, p->in_graph);
+    p->in_graph = false;
     ca_status st = ensure_device(&p->d, &p->cap, total, stream, "plan alloc");
     if (st != CA_OK) return st;
     char* h = nullptr;
@@ -429,7 +446,7 @@ struct ca_cache {
 
   // Tree row -> caller row for a caller order given as seq_ids[0..n) (every
   // live sequence once); uploaded only when it differs from the device copy.
-  ca_status upload_row_map(const int64_t* seq_ids, int64_t n, hipStream_t stream) {
+  ca_status upload_row_map(const int64_t* seq_ids, int64_t n, hipStream_t stream, bool no_upload = false) {
     const size_t B = tables.row_seq.size();
     std::vector<int32_t> map(B, -1);
     for (int64_t i = 0; i < n; ++i) {
@@ -443,6 +460,11 @@ struct ca_cache {
       map[it->second] = static_cast<int32_t>(i);
     }
     if (map == rowmap) return CA_OK;
+    if (no_upload)
+      return fail(CA_ERR_INVALID, "ca_attention: a call that is being captured cannot bring the rows' order up "
+                                  "to date (make one call with it before)");
+    leave_to_graph(&d_rowmap, &d_rowmap_cap, rowmap_in_graph);
+    rowmap_in_graph = false;
     const size_t bytes = std::max<size_t>(B * sizeof(int32_t), 16);
     ca_status st = ensure_device(reinterpret_cast<char**>(&d_rowmap), &d_rowmap_cap, bytes, stream,
                                  "row map alloc");
@@ -473,8 +495,11 @@ struct ca_cache {
   // every launch leaves them at zero again. The first allocation holds what
   // the spread layouts can take (256 KiB), so growing batches and joins do not
   // come back for more, which would wait for the stream.
-  static ca_status ensure_counters(int32_t** p, size_t* cap_, size_t n, hipStream_t stream) {
+  ca_status ensure_counters(int32_t** p, size_t* cap_, size_t n, hipStream_t stream) {
     if (n <= *cap_) return CA_OK;
+    bool& in_graph = p == &d_cnt ? cnt_in_graph : pf_in_graph;
+    leave_to_graph(p, cap_, in_graph);
+    if (p == &d_cnt) in_graph = false;
     hipError_t e;
     if (*p) {
       if ((e = hipStreamSynchronize(stream)) != hipSuccess) return hip_fail(e, "counter sync");
@@ -489,6 +514,11 @@ struct ca_cache {
       return hip_fail(e, "counter clear");
     *cap_ = cap;
     return CA_OK;
+  }
+
+  ca_status ensure_prefill_ws(size_t bytes, hipStream_t stream) {
+    if (bytes > d_pf_ws_cap) leave_to_graph(&d_pf_ws, &d_pf_ws_cap, pf_in_graph);
+    return ensure_device(reinterpret_cast<char**>(&d_pf_ws), &d_pf_ws_cap, bytes, stream, "prefill partials");
   }
 
   // Enqueue K/V copies. Jobs are batched per launch; a job that touches a
@@ -842,16 +872,21 @@ static ca_status plan_attention_impl(ca_cache* cache, const void* q, void* o, co
                                       std::to_string(need) + " bytes");
   const size_t counters = ca::counter_entries(static_cast<size_t>(cache->tree.num_seqs()),
                                               static_cast<size_t>(cache->cfg.num_heads));
-  if ((!slot.uploaded || counters > cache->d_cnt_cap) && capturing(s))
+  const bool graph = capturing(s);
+  if ((!slot.uploaded || counters > cache->d_cnt_cap) && graph)
     return fail(CA_ERR_INVALID, "ca_attention: kernel context not current, and a call that is being "
                                 "captured cannot bring it up to date (prepare, and make one call, before)");
   if (!slot.uploaded && (st = cache->upload_plan(&slot, s)) != CA_OK) return st;
   const int32_t* row_map = nullptr;
   if (seq_ids) {
-    if ((st = cache->upload_row_map(seq_ids, n, s)) != CA_OK) return st;
+    if ((st = cache->upload_row_map(seq_ids, n, s, graph)) != CA_OK) return st;
     row_map = cache->d_rowmap;
   }
-  if ((st = ca_cache::ensure_counters(&cache->d_cnt, &cache->d_cnt_cap, counters, s)) != CA_OK) return st;
+  if ((st = cache->ensure_counters(&cache->d_cnt, &cache->d_cnt_cap, counters, s)) != CA_OK) return st;
+  if (graph) {
+    slot.in_graph = cache->cnt_in_graph = true;
+    if (seq_ids) cache->rowmap_in_graph = true;
+  }
   return launch_plan_call(cache, slot, q, o, scale, static_cast<char*>(ws), cache->d_cnt, row_map, s);
 }
 
@@ -882,7 +917,7 @@ static ca_status attention_impl(ca_cache* cache, const void* q, void* o, float s
     row_map = cache->d_rowmap;
   }
   if (cache->schedule == 3 && (st = cache->ensure_side()) != CA_OK) return st;
-  st = ca_cache::ensure_counters(&cache->d_cnt, &cache->d_cnt_cap,
+  st = cache->ensure_counters(&cache->d_cnt, &cache->d_cnt_cap,
                                  ca::counter_entries(static_cast<size_t>(cache->tree.num_seqs()),
                                                      static_cast<size_t>(cache->cfg.num_heads)),
                                  s);
@@ -990,6 +1025,7 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
                     std::to_string(ca::kScratchBytes - ca::kScratchCounterBytes) +
                     " (use ca_attention with a caller workspace)");
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (plan && capturing(s)) plan->in_graph = true;
   int32_t* cnt = reinterpret_cast<int32_t*>(cache->scratch);
   // the scratch keeps whatever the last call on this GPU left: the counters
   // are cleared by a kernel on the caller's stream before every call
@@ -1156,6 +1192,8 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   int tile_rows = 0;  // of a block; 0: 64, by 16-query wavefronts
   int64_t n_split = 1;
   if (cache->kv4()) {
+    if (!(qscale >= 0x1p-29f && qscale <= 0x1p24f))
+      return fail(CA_ERR_INVALID, std::string(what) + ": a 4-bit cache takes scales from 2^-29 to 2^23 here");
     // Tiles of 128 queries once they give every CU a block: they read each key for
     // twice the queries of a 64-query tile. Below that, tiles of 64 and parts of
     // the keys. The 128-query blocks are four wavefronts (two blocks a CU, so
@@ -1183,7 +1221,8 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   const size_t counters = n_split > 1 ? static_cast<size_t>(tiles) << cnt_shift : 0;
   const size_t path_bytes = hp.size() * sizeof(int32_t);
   const bool inline_path = nc <= ca::kPrefillInlineChunks;
-  if ((!inline_path || ws > cache->d_pf_ws_cap || counters > cache->d_pf_cnt_cap) && capturing(s))
+  const bool graph = capturing(s);
+  if ((!inline_path || ws > cache->d_pf_ws_cap || counters > cache->d_pf_cnt_cap) && graph)
     return fail(CA_ERR_INVALID, std::string(what) + ": a call that is being captured can neither copy a "
                                                     "long path nor grow the partials' memory");
   const int32_t* dpath = nullptr;
@@ -1197,12 +1236,11 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
     dpath = reinterpret_cast<const int32_t*>(cache->d_path);
   }
   if (n_split > 1) {
-    if ((st = ensure_device(reinterpret_cast<char**>(&cache->d_pf_ws), &cache->d_pf_ws_cap, ws, s,
-                            "prefill partials")) != CA_OK)
-      return st;
-    if ((st = ca_cache::ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap, counters, s)) != CA_OK)
+    if ((st = cache->ensure_prefill_ws(ws, s)) != CA_OK) return st;
+    if ((st = cache->ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap, counters, s)) != CA_OK)
       return st;
   }
+  if (graph && n_split > 1) cache->pf_in_graph = true;
   auto common = [&](auto& a) {
     a.H = H;
     a.D = D;
@@ -1340,10 +1378,8 @@ ca_status ca_prefill_attention(ca_cache* cache, int64_t seq_id, const void* q, v
   if (split > 1) {
     const int64_t tiles = (n_q + 63) / 64 * static_cast<int64_t>(a.H);
     const size_t ws = static_cast<size_t>(tiles * split) * ca::prefill_part_bytes(a.D);
-    if ((st = ensure_device(reinterpret_cast<char**>(&cache->d_pf_ws), &cache->d_pf_ws_cap, ws, s,
-                            "prefill partials")) != CA_OK)
-      return st;
-    if ((st = ca_cache::ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap,
+    if ((st = cache->ensure_prefill_ws(ws, s)) != CA_OK) return st;
+    if ((st = cache->ensure_counters(&cache->d_pf_cnt, &cache->d_pf_cnt_cap,
                                         static_cast<size_t>(tiles)
                                             << ca::tile_counter_shift(static_cast<size_t>(tiles)),
                                         s)) != CA_OK)

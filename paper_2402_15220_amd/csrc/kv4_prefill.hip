@@ -30,7 +30,9 @@
 // first rows of one more channel tile of the O product. P's rounding is left.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -67,6 +69,7 @@ struct KwpParams {
   int n_chunks, n_q, H, C, L;
   int window, sinks;
   float qscale;
+  float lq, lv;  // q's and V's factors of log2 r_v: 1 / qscale together, lq a power of two
   int n_split;
   float* ws;
   int32_t* cnt;
@@ -91,22 +94,24 @@ __device__ __forceinline__ half2v codes2(uint32_t w, int pair) {
 }
 
 // A row's parameters: s^, r, 1 / r and b. A row that stands for NaN has s^ = 0
-// and b = NaN. Where 8 s^ would pass fp16's range (a row over nearly all of
-// it), s^ is half and r twice as much.
+// and b = NaN. Where 8 s^ or b / r would pass fp16's range (a row over nearly
+// all of it, or at its ends), s^ is half and r twice as much.
 struct RowPar {
   float s, r, ri, b;
 };
-constexpr float kWideScale = 8000.f;
+constexpr float kWideScale = 8000.f, kFarOff = 32000.f;
 __device__ __forceinline__ RowPar row_par(uint32_t w) {
   const half2v p = __builtin_bit_cast(half2v, w);
   const float s = static_cast<float>(p[0]), low = static_cast<float>(p[1]);
-  const float t = __uint_as_float((__float_as_uint(s > kWideScale ? 0.5f * s : s) + 0x8000u) & 0xffff0000u);
+  const float b = __builtin_fmaf(8.f, s, low);
+  const bool wide = s > kWideScale || __builtin_fabsf(b) > kFarOff;
+  const float t = __uint_as_float((__float_as_uint(wide ? 0.5f * s : s) + 0x8000u) & 0xffff0000u);
   RowPar x;
   const bool on = s > 0.f;  // not 0, not NaN
   x.s = on ? t : 0.f;
   x.r = on ? s * __builtin_amdgcn_rcpf(t) : 1.f;
   x.ri = on ? t * __builtin_amdgcn_rcpf(s) : 1.f;
-  x.b = __builtin_fmaf(8.f, s, low);
+  x.b = b;
   return x;
 }
 
@@ -295,11 +300,10 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
       if (k.r > 1.5f) s_far[ring] = 1;
       *reinterpret_cast<float*>(buf + RK + 4 * r) = P.qscale * k.r;
       // the extra step of the scores, over r_k, by which the product is
-      // multiplied: b_k, and log2 r_v times 2^8 (q's part has 2^-8); a V row
-      // that stands for NaN shows there
+      // multiplied: b_k, and log2 r_v; a V row that stands for NaN shows there
       const float kb = k.b * k.ri;
       const _Float16 hi = static_cast<_Float16>(kb);
-      const float lr = w.b == w.b ? __builtin_amdgcn_logf(w.r) * 256.f * k.ri : w.b;
+      const float lr = w.b == w.b ? __builtin_amdgcn_logf(w.r) * P.lv * k.ri : w.b;
       *reinterpret_cast<half4*>(buf + AU + 8 * r) =
           half4{hi, static_cast<_Float16>(kb - static_cast<float>(hi)), static_cast<_Float16>(lr), hi};
     } else if (g == 1) {
@@ -338,27 +342,29 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
   if (tid == 0) s_far[0] = 0;
   __syncthreads();
 
-  // q's part of the extra step: sum(q) as two fp16 (of q 2^-8, the scores 2^8
-  // back up, where the sum is too large for one), and 2^-8 / qscale
-  float up = 1.f;
+  // q's part of the extra step: sum(q) as two fp16 (of q 2^-8, the query's scores
+  // 2^8 back up, where the sum is too large for one), and lq
+  bool any_up = false;
   {
-    float sum = 0.f;
+    float sum = 0.f, up = 1.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += static_cast<float>(qf[s][i]);
     sum += __shfl_xor(sum, 32);
-    if (__any(fabsf(sum) > 6e4f)) {
-      up = 256.f;
-      sum *= 1.f / 256.f;
+    any_up = __any(fabsf(sum) > 6e4f);
+    if (any_up) {
+      up = fabsf(sum) > 6e4f ? 256.f : 1.f;
+      const float down = 1.f / up;
+      sum *= down;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) qf[s][i] = qf[s][i] * static_cast<_Float16>(1.f / 256.f);
+        for (int i = 0; i < 8; ++i) qf[s][i] = qf[s][i] * static_cast<_Float16>(down);
     }
     const _Float16 hi = static_cast<_Float16>(sum);
     const _Float16 lo = static_cast<_Float16>(sum - static_cast<float>(hi));
-    const _Float16 c = static_cast<_Float16>(fminf(1.f / (P.qscale * up * 256.f), 65504.f));
+    const _Float16 c = static_cast<_Float16>(P.lq / up);
     const _Float16 z = static_cast<_Float16>(0.f);
     qf[KS] = hl == 0 ? half8{hi, hi, c, lo, z, z, z, z} : half8{z, z, z, z, z, z, z, z};
   }
@@ -409,8 +415,11 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
         for (int jt = 0; jt < JT; ++jt)
           sa[jt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[s][jt], qf[s0 + s], sa[jt], 0, 0, 0);
     }
-    if (up != 1.f) {
+    if (any_up) {
       asm volatile("");
+      // the query's 2^8 or 1, from its lane with lq / up (a register of its own
+      // would not be left)
+      const float up = P.lq / __shfl(static_cast<float>(qf[KS][2]), l32);
 #pragma unroll
       for (int jt = 0; jt < JT; ++jt) sa[jt] *= up;
     }
@@ -668,10 +677,16 @@ hipError_t launch_kv4_prefill(const Kv4PrefillArgs& a, hipStream_t stream) {
   if (a.host_path ? a.n_chunks > kPrefillInlineChunks : !a.path) return hipErrorInvalidValue;
   if (a.n_split < 1 || (a.n_split > 1 && (!a.ws || !a.cnt || a.ws_bytes > 0xFFFFFFF0ull)))
     return hipErrorInvalidValue;
+  // lq is a normal fp16 value, exact over 2^8 too; lv log2 r_v (r_v < 2.02) fits
+  // fp16 down to scales of 2^-29, and keeps four bits or more up to 2^24 (log2 r_v
+  // is at most 2^-8 there but for wide rows, so that these are enough)
+  if (!(a.qscale >= 0x1p-29f && a.qscale <= 0x1p24f)) return hipErrorInvalidValue;
+  const float lq = std::ldexp(1.f, std::min(std::max(-std::ilogb(a.qscale) - 8, -13), 14));
   const KwpParams P{static_cast<const _Float16*>(a.q), static_cast<_Float16*>(a.o),
                     static_cast<const char*>(a.kpool), static_cast<const char*>(a.vpool), a.ss, a.hs,
-                    a.path, a.n_chunks, a.n_q, a.H, a.C, a.L, a.window, a.sinks, a.qscale, a.n_split, a.ws,
-                    a.cnt, a.cnt_shift, static_cast<uint32_t>(a.ws_bytes)};
+                    a.path, a.n_chunks, a.n_q, a.H, a.C, a.L, a.window, a.sinks, a.qscale, lq,
+                    1.f / (a.qscale * lq), a.n_split, a.ws, a.cnt, a.cnt_shift,
+                    static_cast<uint32_t>(a.ws_bytes)};
   if (a.D == 128 && a.tile_rows == 128) launch_wp<128, 4, 1, 64>(P, a, stream);
   else if (a.D == 128 && a.tile_rows == 64) launch_wp<128, 2, 4, 32>(P, a, stream);
   else if (a.D == 64 && a.tile_rows == 128) launch_wp<64, 4, 1, 64>(P, a, stream);

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import kv4_quantise
+from oracle import kv4_quantise, kv4_values
 from paper_2402_15220_amd.cache import Cache
 from paper_2402_15220_amd.binding import ChunkAttnError
 from parity_util import assert_close, to_dev
@@ -210,6 +210,100 @@ def test_noalloc_and_graph_replay():
 def _private(p, sid):
     leaf = p.tree.path(sid)[-1]
     return sum(leaf in p.tree.path(s) for s in p.tree.seq_ids()) == 1
+
+
+def _prefill_ref(q, k, v, scale):
+    """Causal, every head, in 64 bits: [n_q, H, d]."""
+    n_q, L = q.shape[0], k.shape[0]
+    s = scale * np.einsum("qhd,lhd->hql", q.astype(np.float64), k)
+    s = np.where(np.arange(L)[None, None] <= (L - n_q + np.arange(n_q))[None, :, None], s, -np.inf)
+    w = np.exp(s - s.max(-1, keepdims=True))
+    return np.einsum("hql,lhd->qhd", w / w.sum(-1, keepdims=True), v)
+
+
+def _prefill_bar(q, k, v, scale, step):
+    """What rounding can do, [n_q, H, 1]. A weight p is rounded to fp16 (2^-11)
+    and scales up to 8 steps of its row (at most `step` each), and o is rounded (2^-11), half a step
+    of the subnormal range where that is larger. A score is the sum of
+    q s^(code - 8) and b sum(q), each at most max|k| sum|q| in size, over d + 8
+    products that fp32 accumulates, off by at most 2^-23 of the running sum at
+    each: e = scale 2 max|k| sum|q| (d + 8) 2^-23, which moves weights by a
+    factor e^(+-2e) and so o by at most 2 e max|v - o| <= 4 e max|v|."""
+    d = q.shape[2]
+    e = scale * 2 * np.abs(k).max() * np.abs(q.astype(np.float64)).sum(-1, keepdims=True) * (d + 8) * 2.0 ** -23
+    return 2.0 ** -11 * (8 * step + np.abs(v).max()) + 4 * e * np.abs(v).max() + 2.0 ** -25
+
+
+def _extreme_rows(rng, n, H, d, kind):
+    x = rng.standard_normal((n, H, d))
+    if kind == "wide":  # some rows over nearly all of fp16's range
+        x[::7] = np.clip(x[::7] * 3e4, -65504, 65504)
+        x[3, :, :2] = (-65504, 65504)
+    elif kind == "end":  # rows at an end of it, and constant ones
+        x[::5] = 65472 + 32 * (rng.random((len(x[::5]), H, d)) > 0.5)
+        x[2::5] = -65504
+    elif kind == "small":  # subnormal values and scales
+        x *= 1e-6
+        x[1::3] *= 0
+    elif kind == "mixed":  # scales over orders of magnitude
+        x *= np.exp2(rng.uniform(-20, 12, (n, H, 1)))
+    return x.astype(np.float16)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("k_kind,v_kind,q_mul,scale", [
+    ("wide", "normal", 1e-4, 0.1), ("end", "normal", 1e-4, 0.1), ("small", "normal", 1e3, 0.1),
+    ("mixed", "normal", 1e-2, 0.1), ("normal", "wide", 1.0, 0.1), ("normal", "end", 1.0, 0.1),
+    ("normal", "small", 1.0, 0.1), ("normal", "mixed", 1.0, 0.1), ("normal", "wide", 1.0, 1e-8),
+    ("normal", "normal", 1e-3, 1e2), ("end", "end", 1e-5, 1.0), ("normal", "normal", 1.0, 50.0)])
+def test_prefill_extremes(d, k_kind, v_kind, q_mul, scale):
+    print(f"[case] kv4 prefill extremes d={d} {k_kind} {v_kind} {q_mul} {scale}", flush=True)
+    rng = np.random.default_rng(21)
+    H, n, n_q = 2, 300, 150
+    p = WPair(64, H, d, "kv4", 16)
+    k, v = _extreme_rows(rng, n, H, d, k_kind), _extreme_rows(rng, n, H, d, v_kind)
+    p.insert(0, np.arange(n, dtype=np.int32), k, v)
+    q = (rng.standard_normal((n_q, H, d)) * q_mul).astype(np.float16)
+    o = p.cache.prefill(0, to_dev(q), scale=scale).cpu().numpy()
+    kk, vv = kv4_values(k).astype(np.float64), kv4_values(v).astype(np.float64)
+    err = np.abs(o - _prefill_ref(q, kk, vv, scale))
+    bar = _prefill_bar(q, kk, vv, scale, kv4_quantise(v)[1].astype(np.float64).max())
+    assert (err <= bar).all(), (err.max(), bar.min())
+
+
+def test_prefill_large_sums_of_q():
+    """Queries whose elements add up to more than fp16 holds, in one tile with
+    queries of ordinary and of tiny elements."""
+    print("[case] kv4 prefill sums of q", flush=True)
+    rng = np.random.default_rng(22)
+    H, d, n = 2, 128, 200
+    for k_mul, scale in ((1.0, 1e-4), (3e3, 1.0)):
+        p = WPair(64, H, d, "kv4", 16)
+        k = (rng.standard_normal((n, H, d)) * k_mul).astype(np.float16)
+        v = rng.standard_normal((n, H, d)).astype(np.float16)
+        p.insert(0, np.arange(n, dtype=np.int32), k, v)
+        q = rng.standard_normal((n, H, d)).astype(np.float16)
+        q[::3] = 1000 + 10 * q[::3]
+        q[1::3] *= np.float16(1e-4)
+        o = p.cache.prefill(0, to_dev(q), scale=scale).cpu().numpy()
+        kk, vv = kv4_values(k).astype(np.float64), kv4_values(v).astype(np.float64)
+        err = np.abs(o - _prefill_ref(q, kk, vv, scale))
+        bar = _prefill_bar(q, kk, vv, scale, kv4_quantise(v)[1].astype(np.float64).max())
+        assert np.isfinite(o).all() and (err <= bar).all(), (err.max(), bar.min())
+        # the tiny ones' bar is their own, not the large ones': sum|q| = 0.0104,
+        # max|k| = 1.4e4: e = 2 * 1.4e4 * 0.0104 * 136 / 2^23 = 4.7e-3, times
+        # 4 max|v| = 17.6 0.083, and the weights' 2^-11 (8 * 0.6 + 4.4) = 0.005
+        assert bar[1::3].max() < 0.1 and (err[1::3] < 0.1).all()
+
+
+def test_prefill_scale_refused():
+    c = Cache(64, 2, 64, 8, kv_bits=4)
+    kv = torch.zeros(4, 2, 64, dtype=torch.float16, device="cuda")
+    c.insert(0, [1, 2, 3, 4], kv, kv)
+    for scale in (1e-12, 1e9, float("nan"), float("inf"), -1.0):
+        with pytest.raises(ChunkAttnError):
+            c.prefill(0, kv, scale=scale)
+    c.close()
 
 
 def test_refusals():

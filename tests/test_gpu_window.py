@@ -160,6 +160,59 @@ def test_graph_replay_follows_appends():
                          *(rng.standard_normal((3, H, d)).astype(p.dtype) for _ in range(2)))
 
 
+def test_graphs_outlive_growth():
+    """Two captured decode calls and a captured prefill of one cache, replayed by
+    turns with eager calls, other windows and joins between, which take the
+    contexts' places and outgrow the workspaces: each replay returns what its
+    call did, and an order of rows not yet uploaded is refused under capture."""
+    print("[case] window graphs outlive growth", flush=True)
+    rng = np.random.default_rng(26)
+    H, d, n_q = 4, 128, 40
+    for kv in ("fp16", "kv4"):
+        p = WPair(64, H, d, kv, 400)
+        new = lambda n: [to_dev(rng.standard_normal((n, H, d)).astype(np.float16)) for _ in range(2)]
+        for s, n in enumerate((700, 1500, 64)):
+            p.cache.insert(s, np.arange(5000 * s, 5000 * s + n), *new(n))
+        q, qp = new(3)[0], new(n_q)[0]
+        ids, other = [2, 0, 1], [1, 0, 2]
+        calls = [lambda o: p.cache.attention(q, out=o, window=600, sinks=2, seq_ids=ids),
+                 lambda o: p.cache.attention(q, out=o, window=10 ** 9, sinks=0),
+                 lambda o: p.cache.prefill(1, qp, out=o, window=1400, sinks=1)]
+        outs = [torch.empty_like(x) for x in (q, q, qp)]
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            want, graphs = [], []
+            for f, o in zip(calls, outs):
+                f(o)
+                want.append(o.clone())
+            torch.cuda.synchronize()
+            for f, o in zip(calls, outs):
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g, stream=stream):
+                    f(o)
+                    if f is calls[0]:
+                        with pytest.raises(ChunkAttnError):
+                            p.cache.attention(q, out=torch.empty_like(q), window=600, sinks=2, seq_ids=other)
+                graphs.append(g)
+            eager = [lambda: p.cache.attention(q, window=600, sinks=2, seq_ids=other),
+                     lambda: (p.cache.attention(q, window=33), p.cache.attention(q, window=44, sinks=7)),
+                     lambda: [p.cache.insert(10 + i, np.arange(10 ** 5 + 900 * i, 10 ** 5 + 900 * i + 800), *new(800))
+                              for i in range(12)],
+                     lambda: (p.cache.attention(torch.zeros(15, H, d, dtype=torch.float16, device="cuda"), window=500),
+                              p.cache.prefill(1, torch.zeros(700, H, d, dtype=torch.float16, device="cuda"),
+                                              window=1400)),
+                     lambda: torch.full((1 << 22,), 0xFF, dtype=torch.uint8, device="cuda")]
+            for step in eager:
+                step()
+                for _ in range(2):
+                    for g, o, w in zip(graphs, outs, want):
+                        o.fill_(float("nan"))
+                        g.replay()
+                        torch.cuda.synchronize()
+                        assert torch.equal(o, w), kv
+
+
 def test_refusals():
     c = Cache(64, 2, 64, 8)
     kv = torch.zeros(4, 2, 64, dtype=torch.float16, device="cuda")
