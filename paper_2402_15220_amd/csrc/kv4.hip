@@ -58,50 +58,67 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
     for (int b0 = first + 16 * blockIdx.z; b0 < end; b0 += 16 * gridDim.z) {
       const int row = b0 + t;  // destination row
       const bool mine = row >= j.dst_pos && row < end;
-      uint32_t kw = 0, vw = 0;  // eight codes, element k at nibble kv4_nibble(k)
+      uint32_t kw = 0;            // K: eight codes, element k at nibble kv4_nibble(k)
+      uint32_t lo4 = 0, hi4 = 0;  // V: eight codes, a byte each
       uint32_t kp = 0, vp = 0;  // (scale, low)
       if (j.kind == 0) {
         const size_t src = ((static_cast<size_t>(j.src) + (mine ? row - j.dst_pos : 0)) * H + h) * D + 8 * e;
         const uint4 kx = *reinterpret_cast<const uint4*>(k + src);
         const uint4 vx = *reinterpret_cast<const uint4*>(v + src);
-        auto quantise = [&](const uint4& raw, uint32_t& word, uint32_t& param) {
+        auto quantise = [&](const uint4& raw, float (&c)[8], uint32_t& param) {
           float x[8];
           Elem<_Float16>::unpack(raw, x);
           float hi = x[0], lo = x[0];
-          bool finite = fabsf(x[0]) < INFINITY;
 #pragma unroll
           for (int i = 1; i < 8; ++i) {
             hi = fmaxf(hi, x[i]);
             lo = fminf(lo, x[i]);
-            finite &= fabsf(x[i]) < INFINITY;
           }
-          if (!finite) hi = INFINITY;  // reaches the whole row through the maximum
+          // NaN where an element is not finite: 0 times it
+          float nan = x[0] * 0.f;
+#pragma unroll
+          for (int i = 1; i < 8; ++i) nan = __builtin_fmaf(x[i], 0.f, nan);
+          if (!(nan == 0.f)) hi = INFINITY;  // reaches the whole row through the maximum
           group_range<LPR>(hi, lo);
           const _Float16 s16 = static_cast<_Float16>((hi - lo) / 15.f);
-          const float s = static_cast<float>(s16);
+          const float s = static_cast<float>(s16), half = 0.5f * s;
           const float inv = s > 0.f ? 1.f / s : 0.f;
-          word = 0;
+          // the nearest code: the product finds it but for a step at a border,
+          // where the residual (exact: few bits) is half a step or more
+          float far = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            // the nearest code, ties to even: the product finds it up to one
-            // step at a border, the residual (exact: few bits) decides
             const float y = x[i] - lo;
-            float c = rintf(y * inv);
-            const float r = 2.f * __builtin_fmaf(-c, s, y);
-            const bool odd = (static_cast<int>(c) & 1) != 0;
-            c += r > s || (odd && r == s) ? 1.f : r < -s || (odd && r == -s) ? -1.f : 0.f;
-            c = s > 0.f ? fminf(fmaxf(c, 0.f), 15.f) : 0.f;
-            word |= static_cast<uint32_t>(c) << (4 * kv4_nibble(i));
+            c[i] = fminf(rintf(y * inv), 15.f);
+            far = fmaxf(far, fabsf(__builtin_fmaf(-c[i], s, y)));
+          }
+          if (far >= half && s > 0.f) {  // decided by the residual, ties to even
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float r = __builtin_fmaf(-c[i], s, x[i] - lo);
+              const bool odd = (static_cast<int>(c[i]) & 1) != 0;
+              c[i] += r > half || (odd && r == half) ? 1.f : r < -half || (odd && r == -half) ? -1.f : 0.f;
+              c[i] = fminf(fmaxf(c[i], 0.f), 15.f);
+            }
           }
           half2v p{s16, static_cast<_Float16>(lo)};
           if (!(hi < INFINITY)) {  // a non-finite element: the row stands for NaN
-            word = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = 0.f;
             p = half2v{static_cast<_Float16>(__builtin_nanf("")), static_cast<_Float16>(__builtin_nanf(""))};
           }
           param = __builtin_bit_cast(uint32_t, p);
         };
-        quantise(kx, kw, kp);
-        quantise(vx, vw, vp);
+        float c[8];
+        quantise(kx, c, kp);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) kw |= static_cast<uint32_t>(c[i]) << (4 * kv4_nibble(i));
+        quantise(vx, c, vp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          lo4 |= static_cast<uint32_t>(c[i]) << (8 * i);
+          hi4 |= static_cast<uint32_t>(c[4 + i]) << (8 * i);
+        }
       } else if (mine) {
         const size_t src = static_cast<size_t>(j.src) * ss + static_cast<size_t>(h) * hs;
         const int sr = j.src_pos + row - j.dst_pos;  // source row
@@ -114,7 +131,7 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t w = words[(16 * ((sr & 15) >> 2) + n0 + i) * (D / 32) + tp];
-          vw |= ((w >> (4 * kv4_nibble(4 * hb + gi))) & 15u) << (4 * kv4_nibble(i));
+          (i < 4 ? lo4 : hi4) |= ((w >> (4 * kv4_nibble(4 * hb + gi))) & 15u) << (8 * (i & 3));
         }
       }
       if (mine) {
@@ -124,12 +141,6 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
           reinterpret_cast<uint32_t*>(vpool + dst + code_bytes)[row] = vp;
         }
       }
-      uint32_t lo4 = 0, hi4 = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        lo4 |= ((vw >> (4 * kv4_nibble(i))) & 15u) << (8 * i);
-        hi4 |= ((vw >> (4 * kv4_nibble(4 + i))) & 15u) << (8 * i);
-      }
       codes[t][2 * e] = lo4;
       codes[t][2 * e + 1] = hi4;
       __syncthreads();
@@ -137,20 +148,19 @@ __global__ __launch_bounds__(2 * D) void kv4_write_kernel(Kv4Jobs b, const _Floa
       {
         const int tp = tid % (D / 32), n = tid / (D / 32) % 16, g = tid / (D / 2);
         uint32_t word = 0, mask = 0;
+        const unsigned char* byte = reinterpret_cast<const unsigned char*>(codes[4 * g]) + 32 * tp + n;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = b0 + 4 * g + i;
           const bool on = r >= j.dst_pos && r < end;
 #pragma unroll
           for (int hb = 0; hb < 2; ++hb) {
-            const int ch = 32 * tp + 16 * hb + n, sh = 4 * kv4_nibble(4 * hb + i);
-            const uint32_t c = (codes[4 * g + i][ch >> 2] >> (8 * (ch & 3))) & 15u;
-            if (on) {
-              word |= c << sh;
-              mask |= 15u << sh;
-            }
+            const int sh = 4 * kv4_nibble(4 * hb + i);
+            word |= static_cast<uint32_t>(byte[i * (D + 4) + 16 * hb]) << sh;
+            mask |= on ? 15u << sh : 0u;
           }
         }
+        word &= mask;
         if (mask) {
           uint32_t* at = reinterpret_cast<uint32_t*>(vpool + dst + static_cast<size_t>(b0) * (D / 2)) + tid;
           *at = mask == 0xffffffffu ? word : (*at & ~mask) | word;
