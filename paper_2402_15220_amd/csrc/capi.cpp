@@ -1194,18 +1194,18 @@ static ca_status window_prefill_impl(ca_cache* cache, int64_t seq_id, const void
   if (cache->kv4()) {
     if (!(qscale >= 0x1p-29f && qscale <= 0x1p24f))
       return fail(CA_ERR_INVALID, std::string(what) + ": a 4-bit cache takes scales from 2^-29 to 2^23 here");
-    // Tiles of 128 queries once they give every CU a block: they read each key for
-    // twice the queries of a 64-query tile. Below that, tiles of 64 and parts of
-    // the keys. The 128-query blocks are four wavefronts (two blocks a CU, so
-    // twice the parts), the 64-query ones eight: with a window of 1,024 and 32
-    // heads of 128, tiles of 64 and of 128 take 64 and 59 us at 1,024 queries, 124
-    // and 74 at 2,048; at 512 tiles of 64 in blocks of four and of eight wavefronts
-    // take 39 and 33. A part is at least two units of keys.
+    // Tiles of 64 queries in blocks of eight wavefronts, one a compute unit, as
+    // long as they fit in one round; then tiles of 128, which turn each key into
+    // operands once for twice the queries, in blocks of four wavefronts, two a
+    // compute unit. Where blocks are left over a tile's keys are cut into parts of
+    // at least two units. 32 heads of 128 behind 1,024 positions, tiles of 64 and of
+    // 128: 256 queries 26.8 and 44.4 us, 512 37.7 and 44.6, 576 64.0 and 52.1, 896
+    // 82.2 and 68.4; 8 heads, 2,560 queries behind 2,048 117 and 86.
     const int64_t cus = cache->num_cus;
-    tile_rows = (n_q + 127) / 128 * H >= cus ? 128 : 64;
+    tile_rows = (n_q + 63) / 64 * H > cus ? 128 : 64;
     const int64_t blocks = (n_q + tile_rows - 1) / tile_rows * H;
     const int64_t keys = std::min<int64_t>(L, seen + tile_rows) + first;
-    const bool wide = tile_rows == 64;  // units of 128 keys, one block a CU
+    const bool wide = tile_rows == 64;  // units of 128 keys
     n_split = std::min<int64_t>(16, std::max<int64_t>(1, std::min<int64_t>((wide ? 1 : 2) * cus / blocks,
                                                                           keys / (wide ? 256 : 128))));
   } else {
