@@ -2,6 +2,7 @@
 #include "plan.hpp"
 
 #include <algorithm>
+#include <numeric>
 
 namespace ca {
 
@@ -95,10 +96,18 @@ void build_plan(const ChunkTree& tree, const Tables& tab, int32_t window, int32_
   }
 
   // Shared runs first: their blocks work on up to 16 rows each; then single
-  // rows, those of a wavefront a head last.
+  // rows, those of a wavefront a head last; of each kind the longest items first,
+  // so that the launch does not end on a long one (128 rows of 64 to 1,024 tokens
+  // of their own behind 2,048 shared ones, 4 bits: in tree order 72.7 us, so 59.0).
+  std::vector<int32_t> order(runs.size());
+  std::iota(order.begin(), order.end(), 0);
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
+    return runs[a].tokens * std::max(1, runs[b].pieces) > runs[b].tokens * std::max(1, runs[a].pieces);
+  });
   for (int pass = 0; pass < 3; ++pass) {
     if (pass == 2) P.n_block_items = static_cast<int32_t>(P.items.size());
-    for (const Run& r : runs) {
+    for (const int32_t at_run : order) {
+      const Run& r = runs[at_run];
       const bool shared = r.row_end - r.row_begin > 1;
       if (pass != (shared ? 0 : r.solo ? 2 : 1)) continue;
       const int32_t n = static_cast<int32_t>(r.seen.size());
