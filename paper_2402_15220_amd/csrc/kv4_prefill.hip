@@ -135,6 +135,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
   constexpr int LDS = 2 * BUF > MB ? 2 * BUF : MB;
   __shared__ __align__(16) char lds[LDS];
   __shared__ int s_last, s_far[4];  // s_far: a unit with a K row of r = 2
+  __shared__ int s_path[INL ? 3 : 1][INL ? (kPrefillInlineChunks + 63) / 64 * 64 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -175,6 +176,11 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
   for (int j0 = 0; 64 * j0 < P.n_chunks; ++j0) {
     const int j = min(64 * j0 + lane, P.n_chunks - 1);
     const int w_start = start_of(j), w_end = end_of(j);
+    if constexpr (INL) {  // every wavefront the same, and reads what it wrote
+      s_path[0][64 * j0 + lane] = slot_of(j);
+      s_path[1][64 * j0 + lane] = w_start;
+      s_path[2][64 * j0 + lane] = w_end;
+    }
     const bool in = 64 * j0 + lane < P.n_chunks;
     const int na = __popcll(__ballot(in && w_start < sinks)), nb = __popcll(__ballot(in && w_end <= blk_lo)),
               ne = __popcll(__ballot(in && w_start <= blk_last));
@@ -204,11 +210,17 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
     const int at = in ? (i < ta ? i : i - ta + tb) : 0;
     const int c = tpc == 1 ? at : static_cast<int>(__umulhi(static_cast<unsigned>(at), magic));
     t_row = (at - c * tpc) * 16;
-    t_slot = slot_of(c);
-    t_pos = start_of(c) + t_row;
-    t_end = in ? min(end_of(c), blk_last + 1) : 0;
-    // wait here, not where the loop reads them
-    asm volatile("" : "+v"(t_slot), "+v"(t_pos), "+v"(t_end));
+    if constexpr (INL) {
+      t_slot = s_path[0][c];
+      t_pos = s_path[1][c] + t_row;
+      t_end = in ? min(s_path[2][c], blk_last + 1) : 0;
+    } else {
+      t_slot = slot_of(c);
+      t_pos = start_of(c) + t_row;
+      t_end = in ? min(end_of(c), blk_last + 1) : 0;
+      // wait here, not where the loop reads them
+      asm volatile("" : "+v"(t_slot), "+v"(t_pos), "+v"(t_end));
+    }
   };
   struct Unit {
     int slot, row, p0, e0;     // of this wavefront's tile (loads, stores)
