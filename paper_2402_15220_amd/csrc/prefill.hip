@@ -113,7 +113,11 @@ using KpfPathOf = std::conditional_t<WIN, KpfWinPath<(NI > 0 ? NI : 1)>, KpfPath
 // operands are looked at (one packed maximum per register), and where there is
 // such an element it counts as 0 and o becomes NaN for the queries that see it:
 // at once in the 16-query blocks; in the 32-query ones, whose loop has no
-// registers left for it, in a second pass over the tile.
+// registers left for it (with it there, 273 were spilled), in a second pass over
+// the tile. 32 heads of 128, 2,048 queries behind 6,144 positions with a window of
+// 4,096: 172 us, 798 TFLOP/s of what is seen; 16 heads of 64, 1,999 queries with one
+// of 333: 14.1 us. A kernel with staged registers and one barrier a unit, without
+// the overlap of kpw_kernel's steps, took 324 and 23.3.
 struct WinUnits {
   int na = 0, nb = 0, ne = 0;  // chunks that start below the sinks; end at or below `lo`; start up to `last`
   int a_start = 0, b_start = 0, e_start = 0;  // starts of chunks na - 1, nb, ne - 1

@@ -6,16 +6,17 @@
 // with j < sinks or j >= L - window:
 //   o = sum_j softmax_j(scale q.k_j) v_j.
 // One block per (item, head): up to 16 query rows over up to 64 chunks that
-// they share, or one row over its own. The four wavefronts take steps of 32
-// tokens (fp32: 16) in turn, each with its own softmax state (m, n, O^T),
-// and are folded (Eqn 2 of the paper) at the end; a row with several items
-// leaves partials, and the last of its blocks to arrive folds them.
+// they share, or one row over its own. The four wavefronts take steps of
+// tokens in turn, each with its own softmax state (m, n, O), and are folded
+// (Eqn 2 of the paper) at the end; a row with several items leaves partials,
+// and the last of its blocks to arrive folds them. Items of single rows that are
+// long and many go a head to a wavefront, four heads to a block (plan.cpp).
 //
-// S^T = K Q^T and O^T += V^T P^T run on the matrix cores with tokens, then
-// channels, as M and query rows as N (a lane holds column n = lane % 16 in
-// its group g = lane / 16), so P stays in the registers S^T came out in:
-// tokens 4g .. 4g + 3 of each 16. A lone row fills one of the 16 columns; its
-// matrix ops still take less of the chip than the memory it waits for.
+// Rows that share (rows_shared): S^T = K Q^T and O^T += V^T P^T run on the
+// matrix cores with tokens, then channels, as M and query rows as N (a lane
+// holds column n = lane % 16 in its group g = lane / 16), so P stays in the
+// registers S^T came out in: tokens 4g .. 4g + 3 of each 16. A single row has
+// loops of its own (row_kv4, row_plain).
 //   fp16   K rows are the A operand as loaded; V rows are turned over through
 //          the wavefront's own LDS tile (ds_read_b64_tr_b16).
 //   fp32   16x16x4 ops; element j of a lane's 16-byte load belongs to op j,
@@ -28,8 +29,21 @@
 //            sum p v = sum (p s_v) (code - 8) + sum p (low_v + 8 s_v);
 //          p s_v is rounded to fp16 for the matrix op, relative to a running
 //          reference of the scales so that it neither overflows nor leaves
-//          the normal range, and the -8 takes the same rounded weights, so
-//          that rounding acts on codes of -8..7 instead of 0..15.
+//          the normal range, and what that rounds off goes in as an operand of
+//          its own, so that P keeps 22 bits; the -8 takes the same weights.
+//
+// What bounds it, and what it takes (32 heads of 128, chunks of 64; the rate is
+// of the bytes that the call has to read): the memory, where rows are many.
+//   fp16, 32 rows, 512 of their 1,024 visible tokens shared     50.1 us  5.5 TB/s
+//   fp16, 16 rows, 2,048 visible tokens of their own            87.0 us  6.2 TB/s
+//   4-bit, 64 rows, 1,024 visible tokens, most of their own     51.2 us  5.5 TB/s
+//   4-bit, 128 rows, 64 to 1,024 tokens behind 2,048 shared     59.0 us  5.3 TB/s
+//   4-bit, 1 row of 32,765 tokens                               26.9 us  5.3 TB/s
+//   4-bit, 32 rows, 512 behind 1,024 shared                     19.5 us  3.9 TB/s
+// (a copy of 2 GiB moves 4.96 TB/s). The last is a round of blocks whose chain of
+// dependent loads (item, length, rows, partials, fold) is most of it, as are
+// calls of a few rows: 8.6 us. In a first version that ran single rows through
+// rows_shared and cut all rows alike the six took 74, 110, 98, 137, 44 and 32 us.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
