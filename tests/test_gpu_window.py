@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2402_15220_amd import binding
 from paper_2402_15220_amd.binding import ChunkAttnError
 from paper_2402_15220_amd.cache import Cache
 from parity_util import assert_close, to_dev
@@ -211,6 +212,46 @@ def test_graphs_outlive_growth():
                         g.replay()
                         torch.cuda.synchronize()
                         assert torch.equal(o, w), kv
+
+
+@pytest.mark.parametrize("kv", KINDS)
+@pytest.mark.parametrize("c", [16, 64])
+def test_far_strides(kv, c):
+    """Slots and heads so far apart that offsets pass 32 bits: every call returns
+    the very values that it returns over dense pools."""
+    print(f"[case] far strides {kv} c={c}", flush=True)
+    rng = np.random.default_rng(27)
+    H, d, L = 2, 128, 30 * c + 5
+    dt = torch.float32 if kv == "fp32" else torch.float16
+    bits = 4 if kv == "kv4" else None
+    near, far = (Cache(c, H, d, 40, dtype=dt, kv_bits=bits) for _ in range(2))
+    # far: K of (slot s, head h) at byte s * 320 MB + h * 100 MB, V 50 MB behind
+    mb = 1 << 20
+    pool = torch.empty(40 * 320 * mb, dtype=torch.uint8, device="cuda")
+    binding.ca_destroy(far.h)
+    es = 1 if bits else near.k_pool.element_size()
+    code = {"fp16": binding.CA_FP16, "fp32": binding.CA_FP32, "kv4": binding.CA_FP16_KV4}[kv]
+    far.h = binding.ca_create(c, H, d, code, 40, pool.data_ptr(), pool.data_ptr() + 50 * mb,
+                              slot_stride=320 * mb // es, head_stride=100 * mb // es)
+    rows = [to_dev(rng.standard_normal((L, H, d))).to(dt) for _ in range(2)]
+    own = [to_dev(rng.standard_normal((70, H, d))).to(dt) for _ in range(2)]
+    q, qp = to_dev(rng.standard_normal((2, H, d))).to(dt), to_dev(rng.standard_normal((300, H, d))).to(dt)
+    got = []
+    for cache in (near, far):
+        cache.insert(0, np.arange(L), *rows)
+        cache.insert(1, np.concatenate([np.arange(L - 100), 10 ** 6 + np.arange(70)]),
+                     *(torch.cat([r[:L - 100], o]) for r, o in zip(rows, own)))
+        outs = [cache.attention(q, window=15 * c, sinks=3), cache.attention(q, window=10 ** 9)]
+        if kv == "kv4":  # (the plain fp32 call may fold its partials in any order)
+            outs.append(cache.attention(q))
+        if kv != "fp32":
+            outs += [cache.prefill(0, qp), cache.prefill(0, qp, window=13 * c, sinks=20), cache.prefill(1, qp[:7])]
+        got.append([o.cpu() for o in outs])
+        torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(*got)):
+        assert torch.isfinite(a).all() and torch.equal(a, b), (i, (a - b).abs().max())
+    near.close()
+    far.close()
 
 
 def test_refusals():
