@@ -100,7 +100,7 @@ typedef enum { CA_FP16 = 0, CA_FP32 = 1, CA_FP16_KV4 = 2 } ca_dtype;
  *               CA_FP16_KV4: strides are in bytes and a tile takes
  *               ceil(c/16) * 16 * (d/2 + 4) bytes in place of c*d elements
  *               (codes, then a scale and a low per row; the arrangement
- *               inside a tile is the library's own).
+ *               inside a tile is the library's own); c <= 16384.
  */
 typedef struct {
   int32_t chunk_size;
@@ -262,7 +262,7 @@ ca_status ca_attention_noalloc(ca_cache* cache, const void* q, void* o, float sc
  *   seq_ids, n   host, the rows' order as in ca_attention_ordered; NULL: tree
  *                row order (n is ignored)
  *   window       >= 1 positions, the query's own among them; sinks >= 0 first
- *                positions that stay visible
+ *                positions that stay visible (caches of chunk_size <= 16384)
  *   ws           device workspace of ws_bytes >= ca_window_workspace_size()
  *                bytes for the same window and sinks, 256-byte aligned
  *   q, o, scale, stream   as ca_attention

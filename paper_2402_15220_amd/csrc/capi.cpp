@@ -565,6 +565,8 @@ const char* ca_last_error(void) { return g_err.c_str(); }
 ca_status ca_create(const ca_config* cfg, ca_cache** out) try {
   if (!cfg || !out) return fail(CA_ERR_INVALID, "ca_create: null argument");
   if (cfg->chunk_size < 1) return fail(CA_ERR_INVALID, "ca_create: chunk_size < 1");
+  if (cfg->dtype == CA_FP16_KV4 && cfg->chunk_size > ca::kWindowChunk)
+    return fail(CA_ERR_INVALID, "ca_create: chunks of more than 16384 tokens in 4 bits");
   if (cfg->num_heads < 1) return fail(CA_ERR_INVALID, "ca_create: num_heads < 1");
   if (cfg->head_dim != 64 && cfg->head_dim != 128)
     return fail(CA_ERR_INVALID, "ca_create: head_dim must be 64 or 128");
@@ -842,9 +844,12 @@ static ca_status launch_plan_call(ca_cache* cache, const PlanSlot& slot, const v
 }
 
 // Window and sinks of a call as a plan holds them.
-static ca_status check_window(int64_t window, int64_t sinks, const char* what, int32_t* w, int32_t* k) {
+static ca_status check_window(const ca_cache* cache, int64_t window, int64_t sinks, const char* what,
+                              int32_t* w, int32_t* k) {
   if (window < 1) return fail(CA_ERR_INVALID, std::string(what) + ": window < 1");
   if (sinks < 0) return fail(CA_ERR_INVALID, std::string(what) + ": sinks < 0");
+  if (cache->cfg.chunk_size > ca::kWindowChunk)
+    return fail(CA_ERR_INVALID, std::string(what) + ": chunks of more than 16384 tokens");
   *w = static_cast<int32_t>(std::min<int64_t>(window, ca::kNoWindow));
   *k = static_cast<int32_t>(std::min<int64_t>(sinks, ca::kNoWindow));
   return CA_OK;
@@ -945,7 +950,7 @@ ca_status ca_window_workspace_size(const ca_cache* cache, int64_t window, int64_
                                    size_t* bytes) try {
   if (!cache || !bytes) return fail(CA_ERR_INVALID, "ca_window_workspace_size: null argument");
   int32_t w = 0, k = 0;
-  ca_status st = check_window(window, sinks, "ca_window_workspace_size", &w, &k);
+  ca_status st = check_window(cache, window, sinks, "ca_window_workspace_size", &w, &k);
   if (st != CA_OK || (st = check_lengths(cache, "ca_window_workspace_size")) != CA_OK) return st;
   ca_cache* c = const_cast<ca_cache*>(cache);
   *bytes = c->plan_ws_bytes(c->ensure_plan(w, k).plan);
@@ -959,7 +964,7 @@ ca_status ca_prepare_window(ca_cache* cache, int64_t window, int64_t sinks, void
   if (uploaded) *uploaded = 0;
   if (!cache) return fail(CA_ERR_INVALID, "ca_prepare_window: null cache");
   int32_t w = 0, k = 0;
-  ca_status st = check_window(window, sinks, "ca_prepare_window", &w, &k);
+  ca_status st = check_window(cache, window, sinks, "ca_prepare_window", &w, &k);
   if (st != CA_OK || (st = check_lengths(cache, "ca_prepare_window")) != CA_OK) return st;
   PlanSlot& slot = cache->ensure_plan(w, k);
   if (cache->table_only || cache->tree.num_seqs() == 0 || slot.uploaded) return CA_OK;
@@ -980,7 +985,7 @@ ca_status ca_attention_window(ca_cache* cache, const void* q, void* o, const int
   if (!cache) return fail(CA_ERR_INVALID, "ca_attention_window: null cache");
   if (cache->table_only) return fail(CA_ERR_INVALID, "ca_attention_window: table-only cache");
   int32_t w = 0, k = 0;
-  ca_status st = check_window(window, sinks, "ca_attention_window", &w, &k);
+  ca_status st = check_window(cache, window, sinks, "ca_attention_window", &w, &k);
   if (st != CA_OK) return st;
   if (seq_ids && n != cache->tree.num_seqs())
     return fail(CA_ERR_INVALID, "ca_attention_window: n differs from the number of live sequences");
@@ -1286,7 +1291,7 @@ ca_status ca_prefill_window(ca_cache* cache, int64_t seq_id, const void* q, void
                             int64_t window, int64_t sinks, float scale, void* stream) try {
   if (!cache) return fail(CA_ERR_INVALID, "ca_prefill_window: null cache");
   int32_t w = 0, k = 0;
-  const ca_status st = check_window(window, sinks, "ca_prefill_window", &w, &k);
+  const ca_status st = check_window(cache, window, sinks, "ca_prefill_window", &w, &k);
   if (st != CA_OK) return st;
   return window_prefill_impl(cache, seq_id, q, o, n_q, w, k, scale, stream, "ca_prefill_window");
 } catch (...) {

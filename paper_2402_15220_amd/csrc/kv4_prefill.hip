@@ -175,7 +175,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
   // Tiles, numbered along the path (chunk * tpc + tile of the chunk):
   // [0, ta) hold the sinks, [tb, te) what the tile's queries see besides.
   const int tpc = (C + 15) >> 4;
-  const uint32_t magic = tpc > 1 ? 0xffffffffu / static_cast<unsigned>(tpc) + 1u : 0u;
+  const uint32_t magic = inverse32(tpc);
   auto slot_of = [&](int j) { if constexpr (INL) return path.slot[j]; else return P.dpath[j]; };
   auto start_of = [&](int j) { if constexpr (INL) return path.start[j]; else return P.dpath[P.n_chunks + j]; };
   auto end_of = [&](int j) { if constexpr (INL) return path.end[j]; else return P.dpath[2 * P.n_chunks + j]; };
@@ -217,7 +217,8 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kwp_kernel(
     const int i = base + lane;
     const bool in = i < n_tiles;
     const int at = in ? (i < ta ? i : i - ta + tb) : 0;
-    const int c = tpc == 1 ? at : static_cast<int>(__umulhi(static_cast<unsigned>(at), magic));
+    int c = divide32(at, tpc, magic);
+    c -= c * tpc > at ? 1 : 0;  // of up to 2^26 tiles
     t_row = (at - c * tpc) * 16;
     if constexpr (INL) {
       t_slot = s_path[0][c];

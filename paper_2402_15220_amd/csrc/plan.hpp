@@ -30,6 +30,10 @@ namespace ca {
 constexpr int kPlanRows = 16;          // rows of an item at most
 constexpr int kPlanChunks = 64;        // chunks of an item at most
 constexpr int32_t kNoWindow = 0x3fffffff;
+// Tokens of a chunk at most: a unit's number (64 tokens, below 2^24 of them in 30
+// bits of positions) times the units of a chunk then stays below 2^32, as the
+// kernels' divisions need.
+constexpr int32_t kWindowChunk = 16384;
 constexpr int32_t kOpenEnd = 0x3fffffff;  // end of a chunk that may still be filled
 
 struct PlanItem {

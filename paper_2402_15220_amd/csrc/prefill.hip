@@ -875,7 +875,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
   // steps of this group whose unit the wavefront sees something of (may be <= 0)
   const int vis_units = CC > 0 ? (n_vis + G - 1) / G : n_vis * upc;
   const int n_see = ((WIN ? wu.seen(vis_units) : vis_units) - grp + KG - 1) / KG;
-  const uint32_t upc_inv = WIN && upc > 1 ? 0xffffffffu / static_cast<unsigned>(upc) + 1u : 0u;
+  const uint32_t upc_inv = WIN ? inverse32(upc) : 0u;
 
   struct Unit {
     int64_t off[G];          // first row of each chunk in a head's pool (elements)
@@ -891,7 +891,7 @@ __global__ __launch_bounds__(64 * QW * KG, 2) void kpw_kernel(KpfParams P, const
     if constexpr (CC > 0) {
       fj = k * G;
     } else {
-      fj = upc == 1 ? k : static_cast<int>(__umulhi(static_cast<unsigned>(k), upc_inv));
+      fj = divide32(k, upc, upc_inv);
       fr = k - fj * upc;
     }
   };

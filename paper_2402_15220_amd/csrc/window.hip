@@ -117,7 +117,7 @@ struct Work {
   PlanChunk my;       // per lane: chunk `lane` of the item
   int nch;            // chunks
   int C, tpc;         // rows and 16-row tiles of a chunk
-  uint32_t magic;     // x / tpc = mul_hi(x, magic) for tpc > 1
+  uint32_t magic;     // inverse32(tpc)
   int n_tiles;
   int sinks, lo_item;
   int len, lo;        // per lane: length and window start of the lane's row
@@ -128,7 +128,7 @@ struct Tile {
 __device__ __forceinline__ Tile tile_at(const Work& W, int i) {  // uniform i
   const bool in = i < W.n_tiles;
   i = in ? i : 0;
-  const int c = W.tpc == 1 ? i : static_cast<int>(__umulhi(static_cast<unsigned>(i), W.magic));
+  const int c = divide32(i, W.tpc, W.magic);
   const int r = (i - c * W.tpc) * 16;
   Tile t;
   t.slot = __builtin_amdgcn_readlane(W.my.slot, c);
@@ -935,7 +935,7 @@ __global__ __launch_bounds__(256, S == kStoreKv4 ? 3 : 2) void kwd_kernel(PlanAr
   W.nch = item.n_chunks;
   W.C = A.C;
   W.tpc = (A.C + 15) >> 4;
-  W.magic = W.tpc > 1 ? 0xffffffffu / static_cast<unsigned>(W.tpc) + 1u : 0u;
+  W.magic = inverse32(W.tpc);
   W.n_tiles = item.n_chunks * W.tpc;
   W.sinks = A.sinks;
   W.lo_item = item.lo;

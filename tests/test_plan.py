@@ -60,6 +60,12 @@ def test_refusals():
         c.prepare(sinks=1)
     with pytest.raises(B.ChunkAttnError):
         B.ca_attention_window(c.h, None, None, None, 4, 0, 0.0, None, 0)
+    big = Cache(16385, 1, 64, 8, table_only=True)
+    with pytest.raises(B.ChunkAttnError):
+        big.prepare(window=5)
+    big.close()
+    with pytest.raises(B.ChunkAttnError):
+        Cache(16385, 1, 64, 8, table_only=True, kv_bits=4)
     # 4-bit tiles: strides are bytes and a tile must fit them
     tile = 64 * 36
     with pytest.raises(B.ChunkAttnError):
