@@ -30,15 +30,6 @@ __device__ __forceinline__ half4 lds_read_tr16(const _Float16* p) {
 
 constexpr float kNegBig = -FLT_MAX;  // "no score yet": exp2(kNegBig - x) == 0, never NaN
 
-// x / n for 0 <= x by a product with the rounded-up inverse; exact while x n
-// stays below 2^32 (windowed calls: kWindowChunk).
-__device__ __forceinline__ uint32_t inverse32(int n) {
-  return n > 1 ? 0xffffffffu / static_cast<unsigned>(n) + 1u : 0u;
-}
-__device__ __forceinline__ int divide32(int x, int n, uint32_t inv) {
-  return n == 1 ? x : static_cast<int>(__umulhi(static_cast<unsigned>(x), inv));
-}
-
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int CTRL>

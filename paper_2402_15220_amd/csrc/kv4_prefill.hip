@@ -46,6 +46,7 @@
 #include <type_traits>
 
 #include "device_common.hpp"
+#include "divide.hpp"
 #include "kernels.hpp"
 #include "kv4.hpp"
 

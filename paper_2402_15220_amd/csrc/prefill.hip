@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "device_common.hpp"
+#include "divide.hpp"
 #include "kernels.hpp"
 
 namespace ca {
