@@ -32,6 +32,7 @@
  *     the hipStream_t passed to the call; callers must use one stream per
  *     cache, which also makes slot reuse after ca_remove safe (later writes
  *     are stream-ordered after earlier reads).
+ *   - The device of the pools must be the current one in every call.
  *   - "host" pointers are read synchronously before the call returns;
  *     "device" pointers must stay valid until the enqueued work completes.
  *   - Tree row order: the query rows q and output rows o are ordered as the
