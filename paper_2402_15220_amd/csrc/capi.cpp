@@ -565,8 +565,6 @@ const char* ca_last_error(void) { return g_err.c_str(); }
 ca_status ca_create(const ca_config* cfg, ca_cache** out) try {
   if (!cfg || !out) return fail(CA_ERR_INVALID, "ca_create: null argument");
   if (cfg->chunk_size < 1) return fail(CA_ERR_INVALID, "ca_create: chunk_size < 1");
-  if (cfg->dtype == CA_FP16_KV4 && cfg->chunk_size > ca::kWindowChunk)
-    return fail(CA_ERR_INVALID, "ca_create: chunks of more than 16384 tokens in 4 bits");
   if (cfg->num_heads < 1) return fail(CA_ERR_INVALID, "ca_create: num_heads < 1");
   if (cfg->head_dim != 64 && cfg->head_dim != 128)
     return fail(CA_ERR_INVALID, "ca_create: head_dim must be 64 or 128");
@@ -577,6 +575,8 @@ ca_status ca_create(const ca_config* cfg, ca_cache** out) try {
     static_assert(sizeof(cfg->dtype) == sizeof(dt), "ca_dtype is a 32-bit enumeration");
     std::memcpy(&dt, &cfg->dtype, sizeof dt);
     if (dt != CA_FP16 && dt != CA_FP32 && dt != CA_FP16_KV4) return fail(CA_ERR_INVALID, "ca_create: bad dtype");
+    if (dt == CA_FP16_KV4 && cfg->chunk_size > ca::kWindowChunk)
+      return fail(CA_ERR_INVALID, "ca_create: chunks of more than 16384 tokens in 4 bits");
   }
   if (cfg->num_slots < 1 || cfg->num_slots > INT32_MAX)
     return fail(CA_ERR_INVALID, "ca_create: num_slots out of range");
